@@ -468,6 +468,52 @@ typedef struct {
 } ts_attention_args;
 ts_status ts_attention_static(const ts_attention_args *a, void *stream);
 
+/* ---- matrices in MXFP4 (microscaled 4-bit floating point) ------------------------------------------ */
+/* Blocks of 32 consecutive elements of a row share a scale 2^(s - 127), s one byte; an element is a sign and one of 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 in four bits (e2m1).  In memory, both contiguous and row-major:
+ *   codes   [rows][nb][16] bytes, nb = ceil(cols / 32): element 2i of a block in the low half of its byte i, 2i + 1 in the high half
+ *   scales  [rows][nb] bytes; 255 makes all elements of the block NaN
+ * Elements of 2^128 and more (scales of 2^126 and 2^127, which ts_mxfp4_quantise never gives) count as infinities.
+ * A row whose length is not a multiple of 32 ends in a block filled up with zeros.  Sides of 0 to 2^21; strides are in elements.
+ * The calls enqueue work on `stream` (a cudaStream_t, 0 = default) of the current device, to which all device pointers
+ * must belong, and return: errors found later surface through the stream.  They allocate nothing and keep nothing from one
+ * call for the next; they can be captured into a CUDA graph.  Errors: TS_ERR_ARG, TS_ERR_CUDA. */
+enum { TS_MX_BF16 = 0, TS_MX_F16 = 1, TS_MX_F32 = 2 };   /* element types of the matrices in 16 or 32 bits */
+
+/* x [rows][cols] (row stride ldx) into codes (16-byte aligned) and scales.  The scale's exponent is floor(log2(largest
+ * magnitude of the block)) - 2, at least -127 (byte 0, which is also the byte of a block of zeros); an element is x / scale rounded
+ * to nearest even, magnitudes above 6 to 6, its sign kept.  A block that holds an infinity or a NaN gets the byte 255 and codes 0. */
+ts_status ts_mxfp4_quantise(const void *x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, void *codes, void *scales,
+                            void *stream);
+/* The values back, rounded to y's type (bf16 and fp32 hold all of them below 2^128): y [rows][cols], row stride ldy; what lies
+ * between the rows of y is left as it is. */
+ts_status ts_mxfp4_dequantise(const void *codes, const void *scales, int64_t rows, int64_t cols, void *y, int32_t y_type,
+                              int64_t ldy, void *stream);
+
+/* The form that ts_mxfp4_product reads a matrix of n rows (output features) and k columns in: blocks of 128 x 128, rows and
+ * columns filled up with zeros.  ts_mxfp4_matrix_bytes: its size (host only).  ts_mxfp4_lay_out: from codes and scales;
+ * matrix: device, 16-byte aligned. */
+ts_status ts_mxfp4_matrix_bytes(int64_t n, int64_t k, uint64_t *bytes);
+ts_status ts_mxfp4_lay_out(const void *codes, const void *scales, int64_t n, int64_t k, void *matrix, void *stream);
+
+/* ts_mxfp4_product: y[m][j] = sum over i of x[m][i] * W[j][i], y [rows][n] with row stride ldy, x [rows][k] with row stride ldx.
+ * Products are exact, sums are fp32; fp16 rows go in as they are and fp32 rows to 16 significant bits (both as a sum of two bf16
+ * numbers).  A row's result depends on that row and on the matrix alone, not on the other rows; up to 64 rows it is the same, bit for
+ * bit, whatever their number.  What lies between the rows of y is left as it is; y must not overlap x or the matrix.
+ * workspace: device, 16-byte aligned, ts_mxfp4_product_workspace bytes (host only call); it may be NULL where x is bf16, 16-byte aligned
+ * and ldx a multiple of 8.  It holds nothing between calls; calls that overlap on the GPU need one each.
+ * status: device, one int32, or NULL: takes a value other than 0 if a wait inside the kernel expired (y is then not valid). */
+typedef struct {
+  int64_t rows, n, k, ldx, ldy;
+  int32_t x_type, y_type;
+  const void *matrix, *x;      /* device */
+  void *y, *workspace;         /* device */
+  uint64_t workspace_bytes;
+  int32_t *status;             /* device */
+} ts_mxfp4_product_args;
+ts_status ts_mxfp4_product_workspace(int64_t rows, int64_t n, int64_t k, int32_t x_type, uint64_t *bytes);
+ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream);
+
 const char *ts_last_error(void);
 
 #ifdef __cplusplus

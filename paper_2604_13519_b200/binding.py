@@ -81,7 +81,20 @@ class ts_attention_args(C.Structure):
                [(n, _P) for n in ("cu_rows", "seq_len", "block_table", "q", "k_pages", "v_pages", "out")]
 
 
+class ts_mxfp4_product_args(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("rows", "n", "k", "ldx", "ldy")] + \
+               [("x_type", C.c_int32), ("y_type", C.c_int32)] + \
+               [(n, _P) for n in ("matrix", "x", "y", "workspace")] + \
+               [("workspace_bytes", C.c_uint64), ("status", _P)]
+
+
 _SIGNATURES = {
+    "ts_mxfp4_quantise": [_P, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _P, _P, _P],
+    "ts_mxfp4_dequantise": [_P, _P, C.c_int64, C.c_int64, _P, C.c_int32, C.c_int64, _P],
+    "ts_mxfp4_matrix_bytes": [C.c_int64, C.c_int64, C.POINTER(C.c_uint64)],
+    "ts_mxfp4_lay_out": [_P, _P, C.c_int64, C.c_int64, _P, _P],
+    "ts_mxfp4_product_workspace": [C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_uint64)],
+    "ts_mxfp4_product": [C.POINTER(ts_mxfp4_product_args), _P],
     "ts_query_buffer_sizes": [C.POINTER(ts_model_config), C.POINTER(ts_buffer_sizes)],
     "ts_init_model": [C.POINTER(ts_model_config), C.POINTER(ts_buffers), _P, C.POINTER(_P)],
     "ts_load_tensor": [_P, C.c_int32, C.c_int32, _P, C.c_int64, C.c_int64],
@@ -607,3 +620,131 @@ def ts_attention_static(q, k_pages, v_pages, block_table, cu_rows: Sequence[int]
     sp = stream.cuda_stream if stream is not None else torch.cuda.current_stream().cuda_stream
     _check(lib().ts_attention_static(C.byref(a), _P(sp)))
     return d_cu, d_len      # keep the device copies alive until the caller has synchronised
+
+
+# ---- matrices in MXFP4 -------------------------------------------------------------------------------
+def _mx_type(dtype):
+    import torch
+    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(dtype)
+    if code is None:
+        raise TypeError(f"{dtype} is not one of bfloat16, float16, float32")
+    return code
+
+
+def _mx_rows(t, name):
+    """A 2-d CUDA tensor whose rows are contiguous: its row stride."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-d CUDA tensor")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return max(t.stride(0), cols) if rows > 1 else cols
+
+
+def _mx_packed(codes, scales, cols):
+    import torch
+    nb = (cols + 31) // 32
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or scales.device != codes.device:
+        raise ValueError("codes and scales must be uint8 tensors on one CUDA device")
+    if codes.dim() != 2 or tuple(codes.shape) != (codes.shape[0], 16 * nb) or tuple(scales.shape) != (codes.shape[0], nb):
+        raise ValueError(f"{cols} columns take codes of [rows][{16 * nb}] and scales of [rows][{nb}]")
+    if not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("codes and scales must be contiguous")
+
+
+class _on_device_of:
+    """The tensor's device made the current one for a call, and the stream to enqueue on (the current one of that device, or the
+    caller's)."""
+
+    def __init__(self, t, stream):
+        import torch
+        self.cuda, self.index, self.stream = torch.cuda, t.device.index, stream
+
+    def __enter__(self):
+        self.before = self.cuda.current_device()
+        if self.before != self.index:
+            self.cuda.set_device(self.index)
+        return _P((self.stream or self.cuda.current_stream()).cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            self.cuda.set_device(self.before)
+
+
+def ts_mxfp4_quantise(x, stream=None):
+    """x: CUDA tensor [rows][cols], bf16, fp16 or fp32, rows contiguous.  Returns (codes uint8 [rows][16 nb], scales uint8
+    [rows][nb]), nb = ceil(cols / 32)."""
+    import torch
+    ldx, (rows, cols) = _mx_rows(x, "x"), x.shape
+    nb = (cols + 31) // 32
+    codes = torch.empty(rows, 16 * nb, dtype=torch.uint8, device=x.device)
+    scales = torch.empty(rows, nb, dtype=torch.uint8, device=x.device)
+    with _on_device_of(x, stream) as sp:
+        _check(lib().ts_mxfp4_quantise(x.data_ptr(), _mx_type(x.dtype), rows, cols, ldx, codes.data_ptr(), scales.data_ptr(), sp))
+    return codes, scales
+
+
+def ts_mxfp4_dequantise(codes, scales, cols: int, dtype, out=None, stream=None):
+    """The values of an MXFP4 matrix of `cols` columns, in `dtype` (bf16, fp16, fp32); written into `out` if it is given."""
+    import torch
+    _mx_packed(codes, scales, cols)
+    y = torch.empty(codes.shape[0], cols, dtype=dtype, device=codes.device) if out is None else out
+    if y.dtype != dtype or tuple(y.shape) != (codes.shape[0], cols) or y.device != codes.device:
+        raise ValueError("out does not match the matrix")
+    ldy = _mx_rows(y, "out")
+    with _on_device_of(codes, stream) as sp:
+        _check(lib().ts_mxfp4_dequantise(codes.data_ptr(), scales.data_ptr(), y.shape[0], cols, y.data_ptr(), _mx_type(dtype), ldy, sp))
+    return y
+
+
+class Mxfp4Matrix:
+    """An MXFP4 matrix [n][k] in the form that ts_mxfp4_product reads, laid out from codes and scales (which it does not keep)."""
+
+    def __init__(self, codes, scales, k: int, stream=None):
+        import torch
+        _mx_packed(codes, scales, k)
+        self.n, self.k, self.device = codes.shape[0], k, codes.device
+        size = C.c_uint64()
+        _check(lib().ts_mxfp4_matrix_bytes(self.n, k, C.byref(size)))
+        self.data = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        with _on_device_of(codes, stream) as sp:
+            _check(lib().ts_mxfp4_lay_out(codes.data_ptr(), scales.data_ptr(), self.n, k, self.data.data_ptr(), sp))
+
+    def workspace(self, rows: int, dtype):
+        """Scratch memory for products of up to `rows` rows of `dtype`, which a caller may keep; one per stream."""
+        import torch
+        size = C.c_uint64()
+        _check(lib().ts_mxfp4_product_workspace(rows, self.n, self.k, _mx_type(dtype), C.byref(size)))
+        return torch.empty(size.value, dtype=torch.uint8, device=self.device)
+
+    def check(self):
+        """Waits for the device and raises if a wait inside a product's kernel has expired since the last check."""
+        code = int(self.status.item())
+        if code:
+            self.status.zero_()
+            raise TsError(-6, f"a bounded device-side wait expired (code {code})")
+
+
+def ts_mxfp4_product(matrix: Mxfp4Matrix, x, dtype=None, out=None, workspace=None, stream=None):
+    """y = x W^T: x CUDA tensor [rows][k], bf16, fp16 or fp32, rows contiguous; y [rows][n] in `dtype` (default: x's), written into `out`
+    if it is given.  workspace: matrix.workspace(rows, x.dtype) or more; made here where it is needed and not given."""
+    import torch
+    ldx, rows = _mx_rows(x, "x"), x.shape[0]
+    if x.shape[1] != matrix.k or x.device != matrix.device:
+        raise ValueError(f"x must have {matrix.k} columns and lie on the matrix's device")
+    if out is None:
+        out = torch.empty(rows, matrix.n, dtype=dtype or x.dtype, device=x.device)
+    elif tuple(out.shape) != (rows, matrix.n) or out.device != x.device or (dtype is not None and out.dtype != dtype):
+        raise ValueError("out does not match the product")
+    a = ts_mxfp4_product_args()
+    a.rows, a.n, a.k, a.ldx, a.ldy = rows, matrix.n, matrix.k, ldx, _mx_rows(out, "out")
+    a.x_type, a.y_type = _mx_type(x.dtype), _mx_type(out.dtype)
+    a.matrix, a.x, a.y, a.status = matrix.data.data_ptr(), x.data_ptr(), out.data_ptr(), matrix.status.data_ptr()
+    if workspace is None and (a.x_type != 0 or ldx % 8 or a.x % 16):
+        workspace = matrix.workspace(rows, x.dtype)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    with _on_device_of(x, stream) as sp:
+        _check(lib().ts_mxfp4_product(C.byref(a), sp))
+    return out

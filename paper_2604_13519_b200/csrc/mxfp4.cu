@@ -1,0 +1,468 @@
+// MXFP4 conversions (quantise, dequantise, the product's storage, activations as bf16 planes) and the entry points of the operators
+// on MXFP4 matrices.  The conversions are bound by memory traffic: one pass, eight elements per thread, 16-byte accesses where
+// alignment allows.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "mxfp4.h"
+#include "toolspec.h"
+
+namespace ts {
+ts_status set_error(ts_status code, const char *fmt, ...);   // model.cu
+int gemm_max_clusters(int cluster, size_t smem_budget);
+
+namespace {
+
+constexpr int kConvThreads = 256, kConvUnroll = 4;   // groups of eight elements: a block's threads take four each
+
+template <int TYPE> struct Elem;
+template <> struct Elem<MX_BF16> { typedef uint16_t raw; };
+template <> struct Elem<MX_F16> { typedef uint16_t raw; };
+template <> struct Elem<MX_F32> { typedef uint32_t raw; };
+template <int TYPE> __device__ __forceinline__ float to_f32(typename Elem<TYPE>::raw r) {
+  if constexpr (TYPE == MX_BF16) return __uint_as_float((uint32_t)r << 16);
+  else if constexpr (TYPE == MX_F16) return __half2float(__ushort_as_half(r));
+  else return __uint_as_float(r);
+}
+template <int TYPE> __device__ __forceinline__ typename Elem<TYPE>::raw from_f32(float v) {
+  if constexpr (TYPE == MX_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+  else if constexpr (TYPE == MX_F16) return __half_as_ushort(__float2half_rn(v));
+  else return __float_as_uint(v);
+}
+
+// elements [c, c + 8) of a row of `cols`, zeros behind its end
+template <int TYPE, bool VEC> __device__ __forceinline__ void load8(const typename Elem<TYPE>::raw *p, int c, int cols, float (&v)[8]) {
+  typedef typename Elem<TYPE>::raw raw;
+  if (VEC && c + 8 <= cols) {
+    __align__(16) raw r[8];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(raw) / 2; ++i) reinterpret_cast<uint4 *>(r)[i] = __ldg(reinterpret_cast<const uint4 *>(p + c) + i);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f32<TYPE>(r[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? to_f32<TYPE>(p[c + i]) : 0.f;
+  }
+}
+
+// Where group u of a block's groups of eight lies: row and first column.  (One 64-bit division per block, 32-bit ones per group.)
+struct Place { long long row; int col; };
+struct Placer {
+  long long row0;
+  uint32_t off, per;
+  __device__ Placer(int groups_per_row) {
+    const long long g0 = (long long)blockIdx.x * (kConvThreads * kConvUnroll);
+    per = groups_per_row;
+    row0 = g0 / per;
+    off = (uint32_t)(g0 - row0 * per);
+  }
+  __device__ Place at(int u) const {
+    const uint32_t l = off + u, r = l / per;
+    return Place{row0 + r, (int)(l - r * per) * 8};
+  }
+};
+
+// Eight fp32 values -> eight e2m1 codes (round to nearest even, saturating), the first in the lowest four bits
+__device__ __forceinline__ uint32_t to_e2m1x8(const float (&v)[8]) {
+  uint32_t d;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(d)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return d;
+}
+// Two codes -> two fp32 values
+__device__ __forceinline__ float2 from_e2m1x2(uint32_t byte) {
+  uint32_t h;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(h) : "r"(byte));
+  return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+}
+
+// Four neighbouring threads share an MX block.  The largest magnitude is found on the bits (a NaN is larger than an infinity, which
+// is larger than all numbers), its exponent field e gives the scale byte: floor(log2) - 2 + 127 = e - 2, at least 0 (numbers below
+// 2^-125 and zeros), 255 where the block has an infinity or NaN.
+template <int TYPE, bool VEC>
+__global__ void __launch_bounds__(kConvThreads)
+mx_quantise_kernel(const typename Elem<TYPE>::raw *x, long long rows, int cols, long long ldx, int nb, uint32_t *codes, uint8_t *scales) {
+  const Placer pl(4 * nb);
+  float v[kConvUnroll][8];
+  Place at[kConvUnroll];
+#pragma unroll
+  for (int i = 0; i < kConvUnroll; ++i) {
+    at[i] = pl.at(i * kConvThreads + threadIdx.x);
+    if (at[i].row < rows) {
+      load8<TYPE, VEC>(x + at[i].row * ldx, at[i].col, cols, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kConvUnroll; ++i) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const uint32_t e = top >> 23, s = e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
+    const float f = __uint_as_float((254u - min(s, 252u)) << 23);   // 2^(127 - s): exact, and no result that matters is subnormal
+    float u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j] = s == 255u ? 0.f : v[i][j] * f;
+    const uint32_t c = to_e2m1x8(u);
+    if (at[i].row < rows) {
+      const long long b = at[i].row * nb + (at[i].col >> 5);
+      codes[b * 4 + ((at[i].col >> 3) & 3)] = c;
+      if ((threadIdx.x & 3) == 0) scales[b] = (uint8_t)s;
+    }
+  }
+}
+
+template <int TYPE, bool VEC>
+__global__ void __launch_bounds__(kConvThreads)
+mx_dequantise_kernel(const uint32_t *codes, const uint8_t *scales, long long rows, int cols, int nb, typename Elem<TYPE>::raw *y, long long ldy) {
+  typedef typename Elem<TYPE>::raw raw;
+  const Placer pl(4 * nb);
+  uint32_t c[kConvUnroll], s[kConvUnroll];
+  Place at[kConvUnroll];
+#pragma unroll
+  for (int i = 0; i < kConvUnroll; ++i) {
+    at[i] = pl.at(i * kConvThreads + threadIdx.x);
+    if (at[i].row >= rows) continue;
+    const long long b = at[i].row * nb + (at[i].col >> 5);
+    c[i] = __ldg(codes + b * 4 + ((at[i].col >> 3) & 3));
+    s[i] = __ldg(scales + b);
+  }
+#pragma unroll
+  for (int i = 0; i < kConvUnroll; ++i) {
+    if (at[i].row >= rows || at[i].col >= cols) continue;
+    // 2^(s - 127); 2^-127 is subnormal
+    const float f = s[i] == 255u ? __uint_as_float(0x7fc00000u) : s[i] == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s[i] << 23);
+    __align__(16) raw r[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 t = from_e2m1x2(c[i] >> (8 * j));
+      r[2 * j] = from_f32<TYPE>(t.x * f);
+      r[2 * j + 1] = from_f32<TYPE>(t.y * f);
+    }
+    raw *d = y + at[i].row * ldy + at[i].col;
+    if (VEC && at[i].col + 8 <= cols) {
+#pragma unroll
+      for (int j = 0; j < (int)sizeof(raw) / 2; ++j) reinterpret_cast<uint4 *>(d)[j] = reinterpret_cast<const uint4 *>(r)[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (at[i].col + j < cols) d[j] = r[j];
+    }
+  }
+}
+
+// One thread per (row, MX block), neighbouring threads on neighbouring rows: 512 contiguous bytes written per warp, 16 read from
+// each of 32 rows.  Rows [n_rows, n_fill) and MX blocks [nb, 4 n_kb) of the storage are filled with zeros.
+__global__ void __launch_bounds__(256)
+mx_lay_out_kernel(const uint4 *codes, const uint8_t *scales, int n_rows, int n_fill, int r0, int nb, int n_kb, RowMap rm, uint8_t *w) {
+  const int i = blockIdx.x * 32 + (threadIdx.x & 31), b = blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (i >= n_fill || b >= 4 * n_kb) return;
+  const int r = r0 + i;
+  int row;
+  if (rm.hd) {
+    const int e = r % rm.hd, half = rm.hd >> 1;
+    row = rm.base + (r / rm.hd) * rm.hd + (e < half ? 2 * e : 2 * (e - half) + 1);
+  } else {
+    row = rm.base + r * rm.mul;
+  }
+  uint32_t out[4] = {0, 0, 0, 0};
+  uint8_t sc = 0;
+  if (i < n_rows && b < nb) {
+    const uint4 c = codes[(size_t)i * nb + b];
+    const uint32_t in[4] = {c.x, c.y, c.z, c.w};
+    sc = scales[(size_t)i * nb + b];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[j] |= mx_place((in[j] >> (4 * e)) & 15u, e >> 1) << (16 * (e & 1));
+  }
+  uint8_t *blk = w + ((size_t)(b >> 2) * rm.tiles + (row >> 7)) * kMxTileBytes;
+  *reinterpret_cast<uint4 *>(blk + (b & 3) * (kMxTileN * 16) + (row & 127) * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+  blk[kMxCodeBytes + (row & 127) * 4 + (b & 3)] = sc;
+}
+
+// x as bf16 planes: the value rounded to bf16, then the remainder.  A finite value beyond bf16's largest keeps to it (and leaves the
+// rest to the next plane); an infinity or NaN has no remainder.
+template <int TYPE, bool VEC>
+__global__ void __launch_bounds__(kConvThreads)
+mx_planes_kernel(const typename Elem<TYPE>::raw *x, long long rows, int cols, long long ldx, __nv_bfloat16 *out, int ldo, int planes) {
+  pdl_launch_dependents();   // (the product waits for this kernel's end before it reads activations)
+  const Placer pl(ldo / 8);
+  const float top = __uint_as_float(0x7f7f0000u);
+#pragma unroll
+  for (int i = 0; i < kConvUnroll; ++i) {
+    const Place at = pl.at(i * kConvThreads + threadIdx.x);
+    if (at.row >= rows) continue;
+    float v[8];
+    load8<TYPE, VEC>(x + at.row * ldx, at.col, cols, v);
+    for (int p = 0; p < planes; ++p) {
+      __align__(16) uint16_t h[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool fin = (__float_as_uint(v[j]) & 0x7f800000u) != 0x7f800000u;
+        const __nv_bfloat16 b = __float2bfloat16_rn(fin ? fminf(fmaxf(v[j], -top), top) : v[j]);
+        h[j] = __bfloat16_as_ushort(b);
+        v[j] = fin ? v[j] - __bfloat162float(b) : 0.f;
+      }
+      *reinterpret_cast<uint4 *>(out + ((size_t)p * rows + at.row) * ldo + at.col) = *reinterpret_cast<const uint4 *>(h);
+    }
+  }
+}
+
+bool aligned(const void *p, long long ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
+unsigned conv_blocks(long long rows, int per_row) {
+  return (unsigned)((rows * per_row + kConvThreads * kConvUnroll - 1) / (kConvThreads * kConvUnroll));
+}
+
+}  // namespace
+
+#define MX_BY_TYPE(type, vec, F)                                                 \
+  switch (type) {                                                                \
+    case MX_BF16: if (vec) F(MX_BF16, true); else F(MX_BF16, false); break;      \
+    case MX_F16: if (vec) F(MX_F16, true); else F(MX_F16, false); break;         \
+    default: if (vec) F(MX_F32, true); else F(MX_F32, false); break;             \
+  }
+
+cudaError_t launch_mx_quantise(const void *x, int type, int rows, int cols, long long ldx, uint8_t *codes, uint8_t *scales, cudaStream_t st) {
+  const int nb = (cols + kMxBlock - 1) / kMxBlock;
+  if (rows <= 0 || cols <= 0) return cudaSuccess;
+  const bool vec = aligned(x, ldx, type == MX_F32 ? 4 : 2);
+#define F(T, V) mx_quantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const Elem<T>::raw *)x, rows, cols, ldx, nb, (uint32_t *)codes, scales)
+  MX_BY_TYPE(type, vec, F)
+#undef F
+  return cudaGetLastError();
+}
+
+cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, int rows, int cols, void *y, int type, long long ldy,
+                                 cudaStream_t st) {
+  const int nb = (cols + kMxBlock - 1) / kMxBlock;
+  if (rows <= 0 || cols <= 0) return cudaSuccess;
+  const bool vec = aligned(y, ldy, type == MX_F32 ? 4 : 2);
+#define F(T, V) mx_dequantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const uint32_t *)codes, scales, rows, cols, nb, (Elem<T>::raw *)y, ldy)
+  MX_BY_TYPE(type, vec, F)
+#undef F
+  return cudaGetLastError();
+}
+
+static cudaError_t lay_out(const uint8_t *codes, const uint8_t *scales, int n_rows, int n_fill, int r0, int nb, RowMap rm, uint8_t *w, cudaStream_t st) {
+  if (n_fill <= 0) return cudaSuccess;
+  const int n_kb = (nb + 3) / 4;
+  mx_lay_out_kernel<<<dim3((n_fill + 31) / 32, (4 * n_kb + 7) / 8), 256, 0, st>>>((const uint4 *)codes, scales, n_rows, n_fill, r0, nb, n_kb, rm, w);
+  return cudaGetLastError();
+}
+cudaError_t launch_mx_lay_out(const uint8_t *codes, const uint8_t *scales, int n_rows, int r0, int nb, RowMap rm, uint8_t *w, cudaStream_t st) {
+  return lay_out(codes, scales, n_rows, n_rows, r0, nb, rm, w, st);
+}
+
+cudaError_t launch_mx_planes(const void *x, int type, int rows, int cols, long long ldx, __nv_bfloat16 *out, int ldo, int planes, cudaStream_t st) {
+  const bool vec = aligned(x, ldx, type == MX_F32 ? 4 : 2);
+#define F(T, V) mx_planes_kernel<T, V><<<conv_blocks(rows, ldo / 8), kConvThreads, 0, st>>>((const Elem<T>::raw *)x, rows, cols, ldx, out, ldo, planes)
+  MX_BY_TYPE(type, vec, F)
+#undef F
+  return cudaGetLastError();
+}
+
+}  // namespace ts
+
+// ---- entry points ---------------------------------------------------------------------------------------------------------------
+namespace {
+
+using ts::set_error;
+
+constexpr int64_t kMostSide = 1 << 21;   // rows and columns of a matrix
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// What a device offers, asked for once per device.
+struct MxDevice {
+  int sms = 0;
+};
+constexpr int kMaxDevices = 64;
+MxDevice g_dev[kMaxDevices];
+std::atomic<uint64_t> g_dev_known{0};
+std::atomic<EncodeTiledFn> g_encode{nullptr};
+
+ts_status device_of_call(MxDevice *out) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return set_error(TS_ERR_CUDA, "cudaGetDevice: %s", cudaGetErrorString(e));
+  if (dev < 0 || dev >= kMaxDevices) return set_error(TS_ERR_ARG, "device ordinal %d not supported", dev);
+  if (!((g_dev_known.load(std::memory_order_acquire) >> dev) & 1)) {
+    int major = 0, sms = 0;
+    e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return set_error(TS_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(e));
+    if (major != 10) return set_error(TS_ERR_CUDA, "device is not an sm_100 part; this library is built for sm_100a only");
+    if (!g_encode.load(std::memory_order_acquire)) {
+      void *fn = nullptr;
+      cudaDriverEntryPointQueryResult q;
+      e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+      if (e != cudaSuccess || !fn || q != cudaDriverEntryPointSuccess) return set_error(TS_ERR_CUDA, "cuTensorMapEncodeTiled not available");
+      g_encode.store((EncodeTiledFn)fn, std::memory_order_release);
+    }
+    g_dev[dev].sms = sms;   // (two threads that come here at once store the same)
+    g_dev_known.fetch_or(1ull << dev, std::memory_order_release);
+  }
+  *out = g_dev[dev];
+  return TS_OK;
+}
+
+bool type_ok(int32_t t) { return t == TS_MX_BF16 || t == TS_MX_F16 || t == TS_MX_F32; }
+size_t type_size(int32_t t) { return t == TS_MX_F32 ? 4 : 2; }
+
+ts_status matrix_ok(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 0 || rows > kMostSide || cols > kMostSide)
+    return set_error(TS_ERR_ARG, "matrix of %lld x %lld: sides must be 0 to %lld", (long long)rows, (long long)cols, (long long)kMostSide);
+  return TS_OK;
+}
+ts_status strided_ok(const char *name, const void *p, int32_t type, int64_t rows, int64_t cols, int64_t ld) {
+  if (!type_ok(type)) return set_error(TS_ERR_ARG, "%s: unknown element type %d", name, type);
+  if (ld < cols) return set_error(TS_ERR_ARG, "%s: row stride %lld is less than the row's %lld elements", name, (long long)ld, (long long)cols);
+  if (rows && cols && !p) return set_error(TS_ERR_ARG, "%s is null", name);
+  if ((uintptr_t)p % type_size(type)) return set_error(TS_ERR_ARG, "%s is not aligned to its elements", name);
+  return TS_OK;
+}
+ts_status packed_ok(const void *codes, const void *scales, int64_t rows, int64_t cols) {
+  if (!rows || !cols) return TS_OK;
+  if (!codes || !scales) return set_error(TS_ERR_ARG, "codes or scales are null");
+  if ((uintptr_t)codes % 16) return set_error(TS_ERR_ARG, "codes must be 16-byte aligned");
+  return TS_OK;
+}
+int planes_of(int32_t type) { return type == TS_MX_BF16 ? 1 : 2; }
+int padded(int64_t k) { return (int)((k + 7) / 8 * 8); }
+uint64_t tiles_of(int64_t n) { return (uint64_t)(n + ts::kMxTileN - 1) / ts::kMxTileN; }
+uint64_t kblocks_of(int64_t k) { return (uint64_t)(k + ts::kMxTileK - 1) / ts::kMxTileK; }
+
+#define MX_TRY(call)                                                                                      \
+  do {                                                                                                    \
+    cudaError_t e_ = (call);                                                                              \
+    if (e_ != cudaSuccess) return set_error(TS_ERR_CUDA, "%s: %s", #call, cudaGetErrorString(e_));        \
+  } while (0)
+#define MX_OK(call)                     \
+  do {                                  \
+    ts_status s_ = (call);              \
+    if (s_ != TS_OK) return s_;         \
+  } while (0)
+
+}  // namespace
+
+extern "C" {
+
+ts_status ts_mxfp4_quantise(const void *x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, void *codes, void *scales, void *stream) {
+  MX_OK(matrix_ok(rows, cols));
+  MX_OK(strided_ok("x", x, x_type, rows, cols, ldx));
+  MX_OK(packed_ok(codes, scales, rows, cols));
+  MxDevice d;
+  MX_OK(device_of_call(&d));
+  MX_TRY(ts::launch_mx_quantise(x, x_type, (int)rows, (int)cols, ldx, (uint8_t *)codes, (uint8_t *)scales, (cudaStream_t)stream));
+  return TS_OK;
+}
+
+ts_status ts_mxfp4_dequantise(const void *codes, const void *scales, int64_t rows, int64_t cols, void *y, int32_t y_type, int64_t ldy, void *stream) {
+  MX_OK(matrix_ok(rows, cols));
+  MX_OK(strided_ok("y", y, y_type, rows, cols, ldy));
+  MX_OK(packed_ok(codes, scales, rows, cols));
+  MxDevice d;
+  MX_OK(device_of_call(&d));
+  MX_TRY(ts::launch_mx_dequantise((const uint8_t *)codes, (const uint8_t *)scales, (int)rows, (int)cols, y, y_type, ldy, (cudaStream_t)stream));
+  return TS_OK;
+}
+
+ts_status ts_mxfp4_matrix_bytes(int64_t n, int64_t k, uint64_t *bytes) {
+  if (!bytes) return set_error(TS_ERR_ARG, "null argument");
+  MX_OK(matrix_ok(n, k));
+  *bytes = tiles_of(n) * kblocks_of(k) * ts::kMxTileBytes;
+  return TS_OK;
+}
+
+ts_status ts_mxfp4_lay_out(const void *codes, const void *scales, int64_t n, int64_t k, void *matrix, void *stream) {
+  MX_OK(matrix_ok(n, k));
+  MX_OK(packed_ok(codes, scales, n, k));
+  if (!n || !k) return TS_OK;
+  if (!matrix || (uintptr_t)matrix % 16) return set_error(TS_ERR_ARG, "matrix is null or not 16-byte aligned");
+  MxDevice d;
+  MX_OK(device_of_call(&d));
+  const int tiles = (int)tiles_of(n);
+  MX_TRY(ts::lay_out((const uint8_t *)codes, (const uint8_t *)scales, (int)n, tiles * ts::kMxTileN, 0, (int)((k + 31) / 32),
+                     ts::RowMap{0, 1, 0, tiles}, (uint8_t *)matrix, (cudaStream_t)stream));
+  return TS_OK;
+}
+
+ts_status ts_mxfp4_product_workspace(int64_t rows, int64_t n, int64_t k, int32_t x_type, uint64_t *bytes) {
+  if (!bytes) return set_error(TS_ERR_ARG, "null argument");
+  MX_OK(matrix_ok(n, k));
+  MX_OK(matrix_ok(rows, k));
+  if (!type_ok(x_type)) return set_error(TS_ERR_ARG, "unknown element type %d", x_type);
+  *bytes = (uint64_t)planes_of(x_type) * rows * padded(k) * 2;
+  return TS_OK;
+}
+
+ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
+  if (!a) return set_error(TS_ERR_ARG, "null argument");
+  const int64_t M = a->rows, N = a->n, K = a->k;
+  MX_OK(matrix_ok(N, K));
+  MX_OK(matrix_ok(M, K));
+  MX_OK(strided_ok("x", a->x, a->x_type, M, K, a->ldx));
+  MX_OK(strided_ok("y", a->y, a->y_type, M, N, a->ldy));
+  if ((uintptr_t)a->status % 4) return set_error(TS_ERR_ARG, "status is not aligned");
+  if (!M || !N) return TS_OK;
+  cudaStream_t st = (cudaStream_t)stream;
+  MxDevice d;
+  MX_OK(device_of_call(&d));
+  if (!K) {   // an empty sum
+    MX_TRY(cudaMemset2DAsync(a->y, a->ldy * type_size(a->y_type), 0, N * type_size(a->y_type), M, st));
+    return TS_OK;
+  }
+  if (!a->matrix || (uintptr_t)a->matrix % 16) return set_error(TS_ERR_ARG, "matrix is null or not 16-byte aligned");
+
+  // The product reads bf16 planes with 16-byte aligned rows: bf16 rows that are, as they are, all others from the workspace.
+  const int planes = planes_of(a->x_type);
+  const bool direct = a->x_type == TS_MX_BF16 && ts::aligned(a->x, a->ldx, 2);
+  void *base = const_cast<void *>(a->x);
+  uint64_t row_bytes = a->ldx * 2;
+  if (!direct) {
+    const uint64_t need = (uint64_t)planes * M * padded(K) * 2;
+    if (!a->workspace || a->workspace_bytes < need || (uintptr_t)a->workspace % 16)
+      return set_error(TS_ERR_ARG, "workspace of %llu bytes, 16-byte aligned, needed for these rows", (unsigned long long)need);
+    MX_TRY(ts::launch_mx_planes(a->x, a->x_type, (int)M, (int)K, a->ldx, (__nv_bfloat16 *)a->workspace, padded(K), planes, st));
+    base = a->workspace;
+    row_bytes = (uint64_t)padded(K) * 2;
+  }
+  ts::MxArgs g{};
+  g.w = (const uint8_t *)a->matrix;
+  g.N = (int)N; g.M = (int)M;
+  g.tiles = (int)tiles_of(N); g.n_kb = (int)kblocks_of(K);
+  g.planes = planes;
+  g.err = a->status;
+  g.y = a->y; g.ldy = a->ldy; g.y_type = a->y_type;
+  const size_t ysz = type_size(a->y_type);
+  g.vec = a->ldy % 4 == 0 && (uintptr_t)a->y % (4 * ysz) == 0;
+  const ts::MxPlan p = ts::mx_plan((int)M, g.tiles, g.n_kb, planes, d.sms);
+  g.Mc = p.Mc;
+  CUtensorMap map;
+  {
+    const cuuint64_t dims[3] = {(cuuint64_t)K, (cuuint64_t)M, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {row_bytes, row_bytes * (cuuint64_t)M};
+    const cuuint32_t box[3] = {64, (cuuint32_t)g.Mc, (cuuint32_t)planes}, es[3] = {1, 1, 1};
+    const CUresult r = g_encode.load(std::memory_order_acquire)(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, es,
+                                                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return set_error(TS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  }
+  MX_TRY(ts::launch_mx_product(ts::MX_STORE, map, g, p.tiles_per_cta, p.cluster, st, true));
+  return TS_OK;
+}
+
+}  // extern "C"

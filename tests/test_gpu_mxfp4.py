@@ -1,0 +1,246 @@
+"""The operators on MXFP4 matrices against their definition in 64 bits (mxfp4_ref)."""
+import numpy as np
+import pytest
+import torch
+
+import mxfp4_ref as ref
+import paper_2604_13519_b200 as ts
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+def _strided(a, dtype, stride):
+    """a (numpy) as the left columns of a wider buffer whose other columns hold 77."""
+    full = torch.full((a.shape[0], stride), 77.0, dtype=dtype, device="cuda")
+    full[:, :a.shape[1]] = torch.from_numpy(np.asarray(a, dtype=np.float64)).to(dtype).cuda()
+    return full, full[:, :a.shape[1]]
+
+
+def _f64(t):
+    return t.double().cpu().numpy()
+
+
+def _matrix(rng, rows, cols):
+    return rng.standard_normal((rows, cols)) * 2.0 ** rng.integers(-6, 7, (rows, 1))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (1, 31, 0), (3, 32, 0), (5, 33, 0), (7, 100, 4), (2, 4096, 0), (129, 250, 6),
+                                           (64, 1024, 8), (1, 8192 + 8, 0), (333, 96, 1)])
+def test_quantise(dtype, rows, cols, pad):
+    rng = np.random.default_rng(rows * 1000 + cols)
+    full, x = _strided(_matrix(rng, rows, cols), TYPES[dtype], cols + pad)
+    codes, scales = ts.ts_mxfp4_quantise(x)
+    want_codes, want_scales = ref.quantise(_f64(x))
+    assert np.array_equal(scales.cpu().numpy(), want_scales)
+    assert np.array_equal(codes.cpu().numpy(), want_codes)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_quantise_borders_and_odd_values(dtype):
+    """Every multiple of a sixteenth up to 8 in blocks of every scale of the type, both signs: all borders between two codes, exactly and
+    next to them; then zeros, the type's smallest and largest numbers, infinities, NaN."""
+    rows = []
+    for e in range(-140, 127, 3):
+        for first in range(0, 129, 31):
+            block = np.arange(first, first + 32) / 16.0
+            block[0] = 7.0
+            rows.append(np.ldexp(block * np.where(np.arange(32) % 3 == 0, -1, 1), e))
+    fin = torch.finfo(TYPES[dtype])
+    for special in ([0.0, -0.0], [fin.max, 1.0], [-fin.max, fin.max * 0.75], [fin.tiny, -fin.tiny / 2], [fin.smallest_normal, 0.0],
+                    [np.inf, 1.0], [-np.inf, 2.0], [np.nan, 3.0], [np.nan, np.inf]):
+        rows.append(np.array(special + [0.0] * 30))
+    _, x = _strided(np.stack(rows), TYPES[dtype], 32)
+    codes, scales = ts.ts_mxfp4_quantise(x)
+    want_codes, want_scales = ref.quantise(_f64(x))
+    assert np.array_equal(scales.cpu().numpy(), want_scales)
+    assert np.array_equal(codes.cpu().numpy(), want_codes)
+
+
+def test_only_the_bad_block_is_lost():
+    x = torch.ones(2, 96, device="cuda")
+    x[0, 40] = float("nan")
+    codes, scales = ts.ts_mxfp4_quantise(x)
+    v = ts.ts_mxfp4_dequantise(codes, scales, 96, torch.float32)
+    assert torch.isnan(v[0, 32:64]).all() and torch.equal(v[0, :32], x[0, :32]) and torch.equal(v[0, 64:], x[0, 64:])
+    assert torch.equal(v[1], x[1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_dequantise_every_code_and_scale(dtype):
+    scales = torch.arange(256, dtype=torch.uint8).view(256, 1).repeat(1, 16).cuda()      # 256 rows, 16 blocks: all code bytes
+    codes = torch.arange(256, dtype=torch.uint8).view(1, 256).repeat(256, 1).cuda()
+    v = ts.ts_mxfp4_dequantise(codes, scales, 512, TYPES[dtype])
+    want = torch.from_numpy(ref.values(codes.cpu().numpy(), scales.cpu().numpy(), 512)).to(TYPES[dtype])
+    assert torch.equal(torch.isnan(v.cpu()), torch.isnan(want))
+    assert torch.equal(v.cpu().nan_to_num(0.5), want.nan_to_num(0.5))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (4, 33, 0), (5, 127, 3), (130, 256, 8)])
+def test_dequantise_into_a_wider_buffer(dtype, rows, cols, pad):
+    rng = np.random.default_rng(rows + cols)
+    codes = torch.from_numpy(rng.integers(0, 256, (rows, 16 * ((cols + 31) // 32)), dtype=np.uint8)).cuda()
+    scales = torch.from_numpy(rng.integers(112, 140, (rows, (cols + 31) // 32), dtype=np.uint8)).cuda()
+    full = torch.full((rows, cols + pad), 77.0, dtype=TYPES[dtype], device="cuda")
+    ts.ts_mxfp4_dequantise(codes, scales, cols, TYPES[dtype], out=full[:, :cols])
+    want = torch.from_numpy(ref.values(codes.cpu().numpy(), scales.cpu().numpy(), cols)).to(TYPES[dtype])
+    assert torch.equal(full[:, :cols].cpu(), want) and (full[:, cols:] == 77).all()
+
+
+def _weights(rng, n, k, lo=112, hi=126):
+    nb = (k + 31) // 32
+    codes = rng.integers(0, 256, (n, 16 * nb), dtype=np.uint8)
+    scales = rng.integers(lo, hi, (n, nb), dtype=np.uint8)
+    return codes, scales, ts.Mxfp4Matrix(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), k)
+
+
+def _check(y, x, w, k, y_dtype, x_dtype):
+    """Products are exact (fp32 rows are taken to within 2^-18 of themselves: two bf16 roundings).  Sums are fp32: an addition is off by at
+    most 2^-23 of what has been added up (truncation), k of them by k 2^-23 of the sum of the magnitudes; then one rounding to y's
+    type, half a step of it (and half of its smallest number, where the result is below its normal ones)."""
+    x, y = _f64(x), _f64(y)
+    want, mag = x @ w.T, np.abs(x) @ np.abs(w).T
+    fin = torch.finfo(y_dtype)
+    room = mag * (k * 2.0 ** -23 + (2.0 ** -18 if x_dtype == torch.float32 else 0.0))
+    room = room + (np.abs(want) + room) * fin.eps / 2 + float(fin.tiny) * fin.eps / 2
+    assert np.isfinite(y).all()
+    assert (np.abs(y - want) <= room).all(), float(np.max(np.abs(y - want) / np.maximum(room, 1e-300)))
+    # and by far not at the edge of that bound where many terms are added: as near as sums of this length are
+    if want.size > 100:
+        assert np.linalg.norm(y - want) <= (fin.eps / 2 + 1e-5) * np.linalg.norm(want) + 1e-30
+
+
+SHAPES = [(1, 1, 1), (1, 128, 128), (1, 129, 33), (2, 100, 32), (3, 256, 160), (8, 128, 1000), (9, 300, 257), (16, 384, 512), (17, 130, 96),
+          (31, 640, 2048), (33, 257, 128), (48, 128, 384), (64, 512, 640), (65, 200, 256), (80, 384, 1024), (127, 129, 520),
+          (128, 256, 256), (129, 640, 192), (200, 1000, 300), (300, 256, 4096), (1, 4096, 4096), (5, 6144, 4096)]
+
+
+@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("x_type,y_type", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("bf16", "f32")])
+def test_product(m, n, k, x_type, y_type):
+    rng = np.random.default_rng(m * 100003 + n * 101 + k)
+    codes, scales, w = _weights(rng, n, k)
+    _, x = _strided(rng.standard_normal((m, k)), TYPES[x_type], k)
+    y = ts.ts_mxfp4_product(w, x, TYPES[y_type])
+    w.check()
+    _check(y, x, ref.values(codes, scales, k), k, TYPES[y_type], TYPES[x_type])
+
+
+@pytest.mark.parametrize("x_type", TYPES)
+@pytest.mark.parametrize("xpad,ypad", [(8, 4), (3, 0), (0, 1), (5, 3)])
+def test_product_of_strided_rows_writes_nothing_beside_them(x_type, xpad, ypad):
+    rng = np.random.default_rng(xpad + 10 * ypad)
+    m, n, k = 19, 200, 264
+    codes, scales, w = _weights(rng, n, k)
+    _, x = _strided(rng.standard_normal((m, k)), TYPES[x_type], k + xpad)
+    full = torch.full((m + 2, n + ypad), 77.0, dtype=TYPES[x_type], device="cuda")
+    ts.ts_mxfp4_product(w, x, out=full[1:m + 1, :n])
+    w.check()
+    assert (full[0] == 77).all() and (full[m + 1] == 77).all() and (full[:, n:] == 77).all()
+    _check(full[1:m + 1, :n], x, ref.values(codes, scales, k), k, TYPES[x_type], TYPES[x_type])
+
+
+def test_product_over_the_whole_range_of_scales():
+    """Scales of 2^-127 to 2^127 in one matrix (a row each, so that no row's sum mixes them), NaN where the byte is 255.  With the
+    bytes 253 and 254 elements of 4 and 6 (and 2, 3) are 2^128 and more: infinities in fp32, in which the sums are."""
+    rng = np.random.default_rng(5)
+    n, k = 256, 128
+    codes = rng.integers(0, 256, (n, 64), dtype=np.uint8)
+    scales = np.repeat(np.arange(256, dtype=np.uint8)[:, None], 4, axis=1)
+    w = ts.Mxfp4Matrix(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), k)
+    x = np.zeros((3, k))
+    x[0], x[1, ::7], x[2] = 2.0 ** -8 * rng.integers(1, 8, k), 0.25, 2.0 ** -9
+    _, xt = _strided(x, torch.bfloat16, k)
+    y = _f64(ts.ts_mxfp4_product(w, xt, torch.float32))
+    with np.errstate(over="ignore", invalid="ignore"):
+        want = x @ ref.values(codes, scales, k).astype(np.float32).astype(np.float64).T
+    assert np.isnan(y[:, 255]).all() and np.isfinite(y[:, :253]).all()
+    assert np.array_equal(np.isnan(y[:, 253:]), np.isnan(want[:, 253:])) and np.array_equal(np.isinf(y[:, 253:]), np.isinf(want[:, 253:]))
+    # all terms of a sum are multiples of one power of two and few: exact in fp32, but for results below its smallest number
+    normal = np.abs(want[:, :253]) >= 2.0 ** -120
+    assert np.array_equal(y[:, :253][normal], want[:, :253][normal])
+    assert np.abs(y[:, :253] - want[:, :253])[~normal].max() <= 2.0 ** -125
+
+
+def test_infinities_and_nan_stay_in_their_rows():
+    rng = np.random.default_rng(6)
+    codes, scales, w = _weights(rng, 200, 256)
+    for dtype in TYPES.values():
+        x = torch.randn(5, 256, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(dtype)
+        good = ts.ts_mxfp4_product(w, x, torch.float32)
+        x[1, 7] = float("inf")
+        x[3, 100] = float("nan")
+        y = ts.ts_mxfp4_product(w, x, torch.float32)
+        assert torch.equal(y[[0, 2, 4]], good[[0, 2, 4]])
+        col = torch.from_numpy(ref.values(codes, scales, 256)[:, 7]).cuda()
+        assert torch.isnan(y[3]).all()
+        assert torch.equal(y[1][col > 0], torch.full_like(y[1][col > 0], float("inf")))
+        assert torch.equal(y[1][col < 0], torch.full_like(y[1][col < 0], -float("inf")))
+        assert torch.isnan(y[1][col == 0]).all()
+
+
+@pytest.mark.parametrize("n,k", [(128, 256), (640, 2048), (4096, 4096), (1000, 777)])
+@pytest.mark.parametrize("x_type", TYPES)
+def test_a_row_s_result_does_not_depend_on_the_others(n, k, x_type):
+    rng = np.random.default_rng(n)
+    _, _, w = _weights(rng, n, k)
+    x = torch.randn(64, k, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(TYPES[x_type])
+    whole = ts.ts_mxfp4_product(w, x, torch.float32)
+    for m in (1, 2, 7, 8, 9, 16, 17, 31, 33, 40, 48, 63):
+        assert torch.equal(ts.ts_mxfp4_product(w, x[:m], torch.float32), whole[:m]), m
+    assert torch.equal(ts.ts_mxfp4_product(w, x[13:14].contiguous(), torch.float32), whole[13:14])
+
+
+def test_empty_sides():
+    e8 = lambda *s: torch.empty(*s, dtype=torch.uint8, device="cuda")
+    w = ts.Mxfp4Matrix(e8(5, 0), e8(5, 0), 0)
+    y = ts.ts_mxfp4_product(w, torch.empty(3, 0, device="cuda"))
+    assert tuple(y.shape) == (3, 5) and (y == 0).all()
+    _, _, w = _weights(np.random.default_rng(0), 5, 32)
+    assert tuple(ts.ts_mxfp4_product(w, torch.empty(0, 32, device="cuda")).shape) == (0, 5)
+    codes, scales = ts.ts_mxfp4_quantise(torch.empty(0, 64, device="cuda"))
+    assert tuple(codes.shape) == (0, 32) and tuple(scales.shape) == (0, 2)
+    assert tuple(ts.ts_mxfp4_dequantise(codes, scales, 64, torch.float32).shape) == (0, 64)
+
+
+def test_captured_and_on_another_stream():
+    rng = np.random.default_rng(8)
+    _, _, w = _weights(rng, 384, 512)
+    x = torch.randn(12, 512, device="cuda")
+    ws, y = w.workspace(12, torch.float32), torch.empty(12, 384, device="cuda")
+    want = ts.ts_mxfp4_product(w, x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ts.ts_mxfp4_product(w, x, out=y, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        codes, scales = ts.ts_mxfp4_quantise(x)
+        back = ts.ts_mxfp4_dequantise(codes, scales, 512, torch.float32)
+        ts.ts_mxfp4_product(w, x, out=y, workspace=ws)
+        z = ts.ts_mxfp4_product(w, back, workspace=ws)
+    for seed in (1, 2):
+        x.copy_(torch.randn(12, 512, generator=torch.Generator().manual_seed(seed)))
+        y.zero_()
+        g.replay()
+        assert torch.equal(y, ts.ts_mxfp4_product(w, x))
+        assert torch.equal(z, ts.ts_mxfp4_product(w, ts.ts_mxfp4_dequantise(*ts.ts_mxfp4_quantise(x), 512, torch.float32)))
+    w.check()
+
+
+def test_quantise_lay_out_multiply_together():
+    """A matrix from bf16 into four bits, laid out and multiplied with: against the matrix's own values in 64 bits, and near the
+    unquantised product (the relative error of an element is at most a quarter, of a sum of many about a tenth)."""
+    rng = np.random.default_rng(9)
+    a = torch.from_numpy(rng.standard_normal((1024, 2048)) * 0.02).to(torch.bfloat16).cuda()
+    codes, scales = ts.ts_mxfp4_quantise(a)
+    w = ts.Mxfp4Matrix(codes, scales, 2048)
+    x = torch.from_numpy(rng.standard_normal((40, 2048))).to(torch.bfloat16).cuda()
+    y = ts.ts_mxfp4_product(w, x, torch.float32)
+    w.check()
+    _check(y, x, ref.values(codes.cpu().numpy(), scales.cpu().numpy(), 2048), 2048, torch.float32, torch.bfloat16)
+    full = _f64(x) @ _f64(a).T
+    assert np.linalg.norm(_f64(y) - full) < 0.25 * np.linalg.norm(full)

@@ -1,0 +1,97 @@
+"""CPU checks of the operators on MXFP4 matrices: refusals, sizes, and the reference that the GPU tests go by."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import mxfp4_ref as ref
+from paper_2604_13519_b200 import binding as B
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    from paper_2604_13519_b200 import build
+    build.build()
+
+
+P = 1 << 20     # an address that is never followed: every call below is refused before any device work
+
+
+def _refused(code, why):
+    assert code == -1, code
+    text = B.lib().ts_last_error().decode()
+    assert why in text, text
+
+
+def test_conversions_refuse():
+    L = B.lib()
+    _refused(L.ts_mxfp4_quantise(P, 3, 4, 64, 64, P, P, None), "element type")
+    _refused(L.ts_mxfp4_quantise(P, 0, -1, 64, 64, P, P, None), "sides")
+    _refused(L.ts_mxfp4_quantise(P, 0, 4, (1 << 21) + 1, 1 << 22, P, P, None), "sides")
+    _refused(L.ts_mxfp4_quantise(P, 0, 4, 64, 63, P, P, None), "stride")
+    _refused(L.ts_mxfp4_quantise(None, 0, 4, 64, 64, P, P, None), "x is null")
+    _refused(L.ts_mxfp4_quantise(P + 1, 0, 4, 64, 64, P, P, None), "aligned")
+    _refused(L.ts_mxfp4_quantise(P + 2, 2, 4, 64, 64, P, P, None), "aligned")
+    _refused(L.ts_mxfp4_quantise(P, 0, 4, 64, 64, P + 8, P, None), "16-byte")
+    _refused(L.ts_mxfp4_quantise(P, 0, 4, 64, 64, P, None, None), "null")
+    _refused(L.ts_mxfp4_dequantise(None, P, 4, 64, P, 0, 64, None), "null")
+    _refused(L.ts_mxfp4_dequantise(P, P, 4, 64, P, 9, 64, None), "element type")
+    _refused(L.ts_mxfp4_dequantise(P, P, 4, 64, None, 0, 64, None), "y is null")
+    _refused(L.ts_mxfp4_lay_out(P, P, 4, 64, None, None), "matrix")
+    _refused(L.ts_mxfp4_lay_out(P, P, 4, 64, P + 4, None), "matrix")
+    _refused(L.ts_mxfp4_matrix_bytes(4, 64, None), "null")
+
+
+def test_product_refuses():
+    L = B.lib()
+    good = dict(rows=4, n=100, k=64, ldx=64, ldy=100, x_type=0, y_type=2, matrix=P, x=P, y=P)
+
+    def call(**over):
+        a = B.ts_mxfp4_product_args()
+        for name, v in {**good, **over}.items():
+            setattr(a, name, v)
+        return L.ts_mxfp4_product(C.byref(a), None)
+
+    _refused(L.ts_mxfp4_product(None, None), "null")
+    _refused(call(x_type=5), "element type")
+    _refused(call(y_type=-1), "element type")
+    _refused(call(rows=-4), "sides")
+    _refused(call(k=1 << 22, ldx=1 << 22), "sides")
+    _refused(call(ldx=60), "stride")
+    _refused(call(ldy=99), "stride")
+    _refused(call(x=None), "x is null")
+    _refused(call(y=None), "y is null")
+    _refused(call(y=P + 2), "aligned")
+    _refused(call(status=P + 2), "status")
+    assert call(rows=0) == 0 and call(n=0, ldy=0) == 0      # nothing to do
+
+
+def test_sizes():
+    L, n = B.lib(), C.c_uint64()
+    size = lambda f, *a: (f(*a, C.byref(n)), n.value)
+    assert size(L.ts_mxfp4_matrix_bytes, 128, 128) == (0, 8704)
+    assert size(L.ts_mxfp4_matrix_bytes, 129, 1) == (0, 2 * 8704)
+    assert size(L.ts_mxfp4_matrix_bytes, 0, 5) == (0, 0)
+    assert size(L.ts_mxfp4_product_workspace, 3, 100, 33, 2)[1] >= 2 * 3 * 40 * 2
+    assert L.ts_mxfp4_product_workspace(3, 100, 33, 7, C.byref(n)) == -1
+
+
+def test_reference_rounds_by_hand():
+    x = np.zeros((1, 32))
+    x[0, :16] = [6, 5, 5.1, 4.9, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25, 0.26, -0.25, -5, 7.9, -7.5, 0]
+    codes, scales = ref.quantise(x)
+    assert scales[0, 0] == 127
+    v = ref.values(codes, scales, 16)[0]
+    assert list(v) == [6, 4, 6, 4, 4, 2, 2, 1, 1, 0, 0.5, 0, -4, 6, -6, 0]
+    assert list(ref.quantise(np.full((1, 1), 2.0 ** -126))[1][0]) == [0]
+    assert list(ref.quantise(np.full((1, 1), np.inf))[1][0]) == [255]
+
+
+def test_binding_refuses():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError):
+        B.ts_mxfp4_quantise(torch.zeros(2, 64))                       # not on a device
+    with pytest.raises(TypeError):
+        B._mx_type(torch.float64)
+    with pytest.raises(ValueError):
+        B._mx_packed(torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.uint8), 64)
