@@ -473,7 +473,6 @@ ts_status ts_attention_static(const ts_attention_args *a, void *stream);
  * 1, 1.5, 2, 3, 4, 6 in four bits (e2m1).  In memory, both contiguous and row-major:
  *   codes   [rows][nb][16] bytes, nb = ceil(cols / 32): element 2i of a block in the low half of its byte i, 2i + 1 in the high half
  *   scales  [rows][nb] bytes; 255 makes all elements of the block NaN
- * Elements of 2^128 and more (scales of 2^126 and 2^127, which ts_mxfp4_quantise never gives) count as infinities.
  * A row whose length is not a multiple of 32 ends in a block filled up with zeros.  Sides of 0 to 2^21; strides are in elements.
  * The calls enqueue work on `stream` (a cudaStream_t, 0 = default) of the current device, to which all device pointers
  * must belong, and return: errors found later surface through the stream.  They allocate nothing and keep nothing from one
@@ -491,22 +490,32 @@ ts_status ts_mxfp4_dequantise(const void *codes, const void *scales, int64_t row
                               int64_t ldy, void *stream);
 
 /* The form that ts_mxfp4_product reads a matrix of n rows (output features) and k columns in: blocks of 128 x 128, rows and
- * columns filled up with zeros.  ts_mxfp4_matrix_bytes: its size (host only).  ts_mxfp4_lay_out: from codes and scales;
- * matrix: device, 16-byte aligned. */
+ * columns filled up with zeros, in device memory of ts_mxfp4_matrix_bytes bytes (host only call), 128-byte aligned.
+ * ts_mxfp4_lay_out writes it from codes and scales; ts_mxfp4_matrix_init describes it for the product (host only; the description
+ * holds its address: a copy elsewhere needs one of its own). */
+typedef struct {
+  int64_t n, k;
+  const void *data;    /* device */
+  uint64_t map[16];    /* for the library */
+} ts_mxfp4_matrix;
 ts_status ts_mxfp4_matrix_bytes(int64_t n, int64_t k, uint64_t *bytes);
-ts_status ts_mxfp4_lay_out(const void *codes, const void *scales, int64_t n, int64_t k, void *matrix, void *stream);
+ts_status ts_mxfp4_lay_out(const void *codes, const void *scales, int64_t n, int64_t k, void *data, void *stream);
+ts_status ts_mxfp4_matrix_init(ts_mxfp4_matrix *m, const void *data, int64_t n, int64_t k);
 
 /* ts_mxfp4_product: y[m][j] = sum over i of x[m][i] * W[j][i], y [rows][n] with row stride ldy, x [rows][k] with row stride ldx.
- * Products are exact, sums are fp32; fp16 rows go in as they are and fp32 rows to 16 significant bits (both as a sum of two bf16
- * numbers).  A row's result depends on that row and on the matrix alone, not on the other rows; up to 64 rows it is the same, bit for
+ * The tensor cores multiply the four-bit elements as they are; x goes in as a sum of 2 (bf16), 3 (fp16) or 5 (fp32) numbers of four
+ * significant bits with a scale per 32 columns, which leaves out less than 2^-20 of the largest of the 32 (of bf16 and fp16 rows
+ * nothing of elements down to 2^-13 of it); sums are fp32.  A row that holds an infinity or a NaN gives NaN.
+ * A row's result depends on that row and on the matrix, not on the other rows: with up to 64 rows (fp32: 32) it is the same, bit for
  * bit, whatever their number.  What lies between the rows of y is left as it is; y must not overlap x or the matrix.
- * workspace: device, 16-byte aligned, ts_mxfp4_product_workspace bytes (host only call); it may be NULL where x is bf16, 16-byte aligned
- * and ldx a multiple of 8.  It holds nothing between calls; calls that overlap on the GPU need one each.
+ * workspace: device, 128-byte aligned, of ts_mxfp4_product_workspace bytes (host only call; enough for fewer rows too).  It holds nothing
+ * between calls; calls that overlap on the GPU need one each.
  * status: device, one int32, or NULL: takes a value other than 0 if a wait inside the kernel expired (y is then not valid). */
 typedef struct {
-  int64_t rows, n, k, ldx, ldy;
+  const ts_mxfp4_matrix *matrix;   /* host, read during the call */
+  int64_t rows, ldx, ldy;
   int32_t x_type, y_type;
-  const void *matrix, *x;      /* device */
+  const void *x;               /* device */
   void *y, *workspace;         /* device */
   uint64_t workspace_bytes;
   int32_t *status;             /* device */

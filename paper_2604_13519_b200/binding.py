@@ -81,10 +81,15 @@ class ts_attention_args(C.Structure):
                [(n, _P) for n in ("cu_rows", "seq_len", "block_table", "q", "k_pages", "v_pages", "out")]
 
 
+class ts_mxfp4_matrix(C.Structure):
+    _fields_ = [("n", C.c_int64), ("k", C.c_int64), ("data", _P), ("map", C.c_uint64 * 16)]
+
+
 class ts_mxfp4_product_args(C.Structure):
-    _fields_ = [(n, C.c_int64) for n in ("rows", "n", "k", "ldx", "ldy")] + \
+    _fields_ = [("matrix", C.POINTER(ts_mxfp4_matrix))] + \
+               [(n, C.c_int64) for n in ("rows", "ldx", "ldy")] + \
                [("x_type", C.c_int32), ("y_type", C.c_int32)] + \
-               [(n, _P) for n in ("matrix", "x", "y", "workspace")] + \
+               [(n, _P) for n in ("x", "y", "workspace")] + \
                [("workspace_bytes", C.c_uint64), ("status", _P)]
 
 
@@ -93,6 +98,7 @@ _SIGNATURES = {
     "ts_mxfp4_dequantise": [_P, _P, C.c_int64, C.c_int64, _P, C.c_int32, C.c_int64, _P],
     "ts_mxfp4_matrix_bytes": [C.c_int64, C.c_int64, C.POINTER(C.c_uint64)],
     "ts_mxfp4_lay_out": [_P, _P, C.c_int64, C.c_int64, _P, _P],
+    "ts_mxfp4_matrix_init": [C.POINTER(ts_mxfp4_matrix), _P, C.c_int64, C.c_int64],
     "ts_mxfp4_product_workspace": [C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.POINTER(C.c_uint64)],
     "ts_mxfp4_product": [C.POINTER(ts_mxfp4_product_args), _P],
     "ts_query_buffer_sizes": [C.POINTER(ts_model_config), C.POINTER(ts_buffer_sizes)],
@@ -623,22 +629,27 @@ def ts_attention_static(q, k_pages, v_pages, block_table, cu_rows: Sequence[int]
 
 
 # ---- matrices in MXFP4 -------------------------------------------------------------------------------
+_mx_types = {}
+
+
 def _mx_type(dtype):
-    import torch
-    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(dtype)
+    if not _mx_types:
+        import torch
+        _mx_types.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+    code = _mx_types.get(dtype)
     if code is None:
         raise TypeError(f"{dtype} is not one of bfloat16, float16, float32")
     return code
 
 
 def _mx_rows(t, name):
-    """A 2-d CUDA tensor whose rows are contiguous: its row stride."""
+    """A 2-d CUDA tensor whose rows are contiguous: rows, columns, row stride."""
     if not t.is_cuda or t.dim() != 2:
         raise ValueError(f"{name} must be a 2-d CUDA tensor")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have contiguous rows")
-    return max(t.stride(0), cols) if rows > 1 else cols
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if cols > 1 and step != 1 or rows > 1 and ld < cols:
+        raise ValueError(f"{name} must have rows that are contiguous and do not overlap")
+    return rows, cols, ld if rows > 1 else cols
 
 
 def _mx_packed(codes, scales, cols):
@@ -652,35 +663,27 @@ def _mx_packed(codes, scales, cols):
         raise ValueError("codes and scales must be contiguous")
 
 
-class _on_device_of:
-    """The tensor's device made the current one for a call, and the stream to enqueue on (the current one of that device, or the
-    caller's)."""
-
-    def __init__(self, t, stream):
-        import torch
-        self.cuda, self.index, self.stream = torch.cuda, t.device.index, stream
-
-    def __enter__(self):
-        self.before = self.cuda.current_device()
-        if self.before != self.index:
-            self.cuda.set_device(self.index)
-        return _P((self.stream or self.cuda.current_stream()).cuda_stream)
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            self.cuda.set_device(self.before)
+def _on_device_of(index, stream, call, *args):
+    """call(*args, stream) with device `index` the current one, on `stream` or that device's current stream."""
+    import torch
+    before = torch.cuda.current_device()
+    if before == index:
+        _check(call(*args, stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)))
+        return
+    with torch.cuda.device(index):
+        _check(call(*args, stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)))
 
 
 def ts_mxfp4_quantise(x, stream=None):
     """x: CUDA tensor [rows][cols], bf16, fp16 or fp32, rows contiguous.  Returns (codes uint8 [rows][16 nb], scales uint8
     [rows][nb]), nb = ceil(cols / 32)."""
     import torch
-    ldx, (rows, cols) = _mx_rows(x, "x"), x.shape
+    rows, cols, ldx = _mx_rows(x, "x")
     nb = (cols + 31) // 32
     codes = torch.empty(rows, 16 * nb, dtype=torch.uint8, device=x.device)
     scales = torch.empty(rows, nb, dtype=torch.uint8, device=x.device)
-    with _on_device_of(x, stream) as sp:
-        _check(lib().ts_mxfp4_quantise(x.data_ptr(), _mx_type(x.dtype), rows, cols, ldx, codes.data_ptr(), scales.data_ptr(), sp))
+    _on_device_of(x.device.index, stream, lib().ts_mxfp4_quantise, x.data_ptr(), _mx_type(x.dtype), rows, cols, ldx, codes.data_ptr(),
+                  scales.data_ptr())
     return codes, scales
 
 
@@ -691,9 +694,9 @@ def ts_mxfp4_dequantise(codes, scales, cols: int, dtype, out=None, stream=None):
     y = torch.empty(codes.shape[0], cols, dtype=dtype, device=codes.device) if out is None else out
     if y.dtype != dtype or tuple(y.shape) != (codes.shape[0], cols) or y.device != codes.device:
         raise ValueError("out does not match the matrix")
-    ldy = _mx_rows(y, "out")
-    with _on_device_of(codes, stream) as sp:
-        _check(lib().ts_mxfp4_dequantise(codes.data_ptr(), scales.data_ptr(), y.shape[0], cols, y.data_ptr(), _mx_type(dtype), ldy, sp))
+    rows, _, ldy = _mx_rows(y, "out")
+    _on_device_of(codes.device.index, stream, lib().ts_mxfp4_dequantise, codes.data_ptr(), scales.data_ptr(), rows, cols, y.data_ptr(),
+                  _mx_type(dtype), ldy)
     return y
 
 
@@ -703,13 +706,16 @@ class Mxfp4Matrix:
     def __init__(self, codes, scales, k: int, stream=None):
         import torch
         _mx_packed(codes, scales, k)
-        self.n, self.k, self.device = codes.shape[0], k, codes.device
+        self.n, self.k, self.device, self.index = codes.shape[0], k, codes.device, codes.device.index
         size = C.c_uint64()
         _check(lib().ts_mxfp4_matrix_bytes(self.n, k, C.byref(size)))
         self.data = torch.empty(size.value, dtype=torch.uint8, device=self.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        with _on_device_of(codes, stream) as sp:
-            _check(lib().ts_mxfp4_lay_out(codes.data_ptr(), scales.data_ptr(), self.n, k, self.data.data_ptr(), sp))
+        self.handle = ts_mxfp4_matrix()
+        with torch.cuda.device(self.index):
+            _check(lib().ts_mxfp4_matrix_init(C.byref(self.handle), self.data.data_ptr(), self.n, k))
+        self._status_ptr, self._handle_ref = self.status.data_ptr(), C.pointer(self.handle)
+        _on_device_of(self.index, stream, lib().ts_mxfp4_lay_out, codes.data_ptr(), scales.data_ptr(), self.n, k, self.data.data_ptr())
 
     def workspace(self, rows: int, dtype):
         """Scratch memory for products of up to `rows` rows of `dtype`, which a caller may keep; one per stream."""
@@ -728,23 +734,24 @@ class Mxfp4Matrix:
 
 def ts_mxfp4_product(matrix: Mxfp4Matrix, x, dtype=None, out=None, workspace=None, stream=None):
     """y = x W^T: x CUDA tensor [rows][k], bf16, fp16 or fp32, rows contiguous; y [rows][n] in `dtype` (default: x's), written into `out`
-    if it is given.  workspace: matrix.workspace(rows, x.dtype) or more; made here where it is needed and not given."""
+    if it is given.  workspace: matrix.workspace(rows, x.dtype) or more; made here if it is not given."""
     import torch
-    ldx, rows = _mx_rows(x, "x"), x.shape[0]
-    if x.shape[1] != matrix.k or x.device != matrix.device:
+    rows, cols, ldx = _mx_rows(x, "x")
+    if cols != matrix.k or x.device != matrix.device:
         raise ValueError(f"x must have {matrix.k} columns and lie on the matrix's device")
+    n = matrix.n
     if out is None:
-        out = torch.empty(rows, matrix.n, dtype=dtype or x.dtype, device=x.device)
-    elif tuple(out.shape) != (rows, matrix.n) or out.device != x.device or (dtype is not None and out.dtype != dtype):
-        raise ValueError("out does not match the product")
-    a = ts_mxfp4_product_args()
-    a.rows, a.n, a.k, a.ldx, a.ldy = rows, matrix.n, matrix.k, ldx, _mx_rows(out, "out")
-    a.x_type, a.y_type = _mx_type(x.dtype), _mx_type(out.dtype)
-    a.matrix, a.x, a.y, a.status = matrix.data.data_ptr(), x.data_ptr(), out.data_ptr(), matrix.status.data_ptr()
-    if workspace is None and (a.x_type != 0 or ldx % 8 or a.x % 16):
+        out = torch.empty((rows, n), dtype=dtype or x.dtype, device=matrix.device)
+        ldy = n
+    else:
+        have, width, ldy = _mx_rows(out, "out")
+        if (have, width) != (rows, n) or out.device != matrix.device or (dtype is not None and out.dtype != dtype):
+            raise ValueError("out does not match the product")
+    if workspace is None:
         workspace = matrix.workspace(rows, x.dtype)
-    if workspace is not None:
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    with _on_device_of(x, stream) as sp:
-        _check(lib().ts_mxfp4_product(C.byref(a), sp))
+    elif workspace.device != matrix.device:
+        raise ValueError("the workspace must lie on the matrix's device")
+    a = ts_mxfp4_product_args(matrix._handle_ref, rows, ldx, ldy, _mx_type(x.dtype), _mx_type(out.dtype), x.data_ptr(), out.data_ptr(),
+                              workspace.data_ptr(), workspace.numel() * workspace.element_size(), matrix._status_ptr)
+    _on_device_of(matrix.index, stream, lib().ts_mxfp4_product, C.byref(a))
     return out

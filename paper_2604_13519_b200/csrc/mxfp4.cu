@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cstring>
 
 #include "mxfp4.h"
 #include "toolspec.h"
@@ -16,36 +17,6 @@ int gemm_max_clusters(int cluster, size_t smem_budget);
 namespace {
 
 constexpr int kConvThreads = 256, kConvUnroll = 4;   // groups of eight elements: a block's threads take four each
-
-template <int TYPE> struct Elem;
-template <> struct Elem<MX_BF16> { typedef uint16_t raw; };
-template <> struct Elem<MX_F16> { typedef uint16_t raw; };
-template <> struct Elem<MX_F32> { typedef uint32_t raw; };
-template <int TYPE> __device__ __forceinline__ float to_f32(typename Elem<TYPE>::raw r) {
-  if constexpr (TYPE == MX_BF16) return __uint_as_float((uint32_t)r << 16);
-  else if constexpr (TYPE == MX_F16) return __half2float(__ushort_as_half(r));
-  else return __uint_as_float(r);
-}
-template <int TYPE> __device__ __forceinline__ typename Elem<TYPE>::raw from_f32(float v) {
-  if constexpr (TYPE == MX_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
-  else if constexpr (TYPE == MX_F16) return __half_as_ushort(__float2half_rn(v));
-  else return __float_as_uint(v);
-}
-
-// elements [c, c + 8) of a row of `cols`, zeros behind its end
-template <int TYPE, bool VEC> __device__ __forceinline__ void load8(const typename Elem<TYPE>::raw *p, int c, int cols, float (&v)[8]) {
-  typedef typename Elem<TYPE>::raw raw;
-  if (VEC && c + 8 <= cols) {
-    __align__(16) raw r[8];
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(raw) / 2; ++i) reinterpret_cast<uint4 *>(r)[i] = __ldg(reinterpret_cast<const uint4 *>(p + c) + i);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_f32<TYPE>(r[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? to_f32<TYPE>(p[c + i]) : 0.f;
-  }
-}
 
 // Where group u of a block's groups of eight lies: row and first column.  (One 64-bit division per block, 32-bit ones per group.)
 struct Place { long long row; int col; };
@@ -87,7 +58,7 @@ __device__ __forceinline__ float2 from_e2m1x2(uint32_t byte) {
 // 2^-125 and zeros), 255 where the block has an infinity or NaN.
 template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(kConvThreads)
-mx_quantise_kernel(const typename Elem<TYPE>::raw *x, long long rows, int cols, long long ldx, int nb, uint32_t *codes, uint8_t *scales) {
+mx_quantise_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols, long long ldx, int nb, uint32_t *codes, uint8_t *scales) {
   const Placer pl(4 * nb);
   float v[kConvUnroll][8];
   Place at[kConvUnroll];
@@ -95,7 +66,7 @@ mx_quantise_kernel(const typename Elem<TYPE>::raw *x, long long rows, int cols, 
   for (int i = 0; i < kConvUnroll; ++i) {
     at[i] = pl.at(i * kConvThreads + threadIdx.x);
     if (at[i].row < rows) {
-      load8<TYPE, VEC>(x + at[i].row * ldx, at[i].col, cols, v[i]);
+      mx_load8<TYPE>(x + at[i].row * ldx, true, at[i].col, cols, VEC, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
@@ -124,8 +95,8 @@ mx_quantise_kernel(const typename Elem<TYPE>::raw *x, long long rows, int cols, 
 
 template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(kConvThreads)
-mx_dequantise_kernel(const uint32_t *codes, const uint8_t *scales, long long rows, int cols, int nb, typename Elem<TYPE>::raw *y, long long ldy) {
-  typedef typename Elem<TYPE>::raw raw;
+mx_dequantise_kernel(const uint32_t *codes, const uint8_t *scales, long long rows, int cols, int nb, typename MxElem<TYPE>::raw *y, long long ldy) {
+  typedef typename MxElem<TYPE>::raw raw;
   const Placer pl(4 * nb);
   uint32_t c[kConvUnroll], s[kConvUnroll];
   Place at[kConvUnroll];
@@ -146,8 +117,8 @@ mx_dequantise_kernel(const uint32_t *codes, const uint8_t *scales, long long row
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 t = from_e2m1x2(c[i] >> (8 * j));
-      r[2 * j] = from_f32<TYPE>(t.x * f);
-      r[2 * j + 1] = from_f32<TYPE>(t.y * f);
+      r[2 * j] = mx_from_f32<TYPE>(t.x * f);
+      r[2 * j + 1] = mx_from_f32<TYPE>(t.y * f);
     }
     raw *d = y + at[i].row * ldy + at[i].col;
     if (VEC && at[i].col + 8 <= cols) {
@@ -161,11 +132,11 @@ mx_dequantise_kernel(const uint32_t *codes, const uint8_t *scales, long long row
   }
 }
 
-// One thread per (row, MX block), neighbouring threads on neighbouring rows: 512 contiguous bytes written per warp, 16 read from
-// each of 32 rows.  Rows [n_rows, n_fill) and MX blocks [nb, 4 n_kb) of the storage are filled with zeros.
+// One thread per (row, MX block), four neighbouring threads on a row's 64 bytes of a block.  Rows [n_rows, n_fill) and MX blocks
+// [nb, 4 n_kb) of the storage are filled with zeros.
 __global__ void __launch_bounds__(256)
 mx_lay_out_kernel(const uint4 *codes, const uint8_t *scales, int n_rows, int n_fill, int r0, int nb, int n_kb, RowMap rm, uint8_t *w) {
-  const int i = blockIdx.x * 32 + (threadIdx.x & 31), b = blockIdx.y * 8 + (threadIdx.x >> 5);
+  const int i = blockIdx.x * 32 + (threadIdx.x >> 3), b = blockIdx.y * 8 + (threadIdx.x & 7);
   if (i >= n_fill || b >= 4 * n_kb) return;
   const int r = r0 + i;
   int row;
@@ -175,48 +146,28 @@ mx_lay_out_kernel(const uint4 *codes, const uint8_t *scales, int n_rows, int n_f
   } else {
     row = rm.base + r * rm.mul;
   }
-  uint32_t out[4] = {0, 0, 0, 0};
-  uint8_t sc = 0;
-  if (i < n_rows && b < nb) {
-    const uint4 c = codes[(size_t)i * nb + b];
-    const uint32_t in[4] = {c.x, c.y, c.z, c.w};
-    sc = scales[(size_t)i * nb + b];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) out[j] |= mx_place((in[j] >> (4 * e)) & 15u, e >> 1) << (16 * (e & 1));
-  }
-  uint8_t *blk = w + ((size_t)(b >> 2) * rm.tiles + (row >> 7)) * kMxTileBytes;
-  *reinterpret_cast<uint4 *>(blk + (b & 3) * (kMxTileN * 16) + (row & 127) * 16) = make_uint4(out[0], out[1], out[2], out[3]);
-  blk[kMxCodeBytes + (row & 127) * 4 + (b & 3)] = sc;
+  const bool there = i < n_rows && b < nb;
+  uint8_t *blk = w + (size_t)mx_block(row >> 7, b >> 2, n_kb) * kMxTileBytes;
+  *reinterpret_cast<uint4 *>(blk + (row & 127) * 64 + (b & 3) * 16) = there ? codes[(size_t)i * nb + b] : make_uint4(0, 0, 0, 0);
+  blk[mx_scale_at(row & 127) + (b & 3)] = there ? scales[(size_t)i * nb + b] : 0;
 }
 
-// x as bf16 planes: the value rounded to bf16, then the remainder.  A finite value beyond bf16's largest keeps to it (and leaves the
-// rest to the next plane); an infinity or NaN has no remainder.
 template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(kConvThreads)
-mx_planes_kernel(const typename Elem<TYPE>::raw *x, long long rows, int cols, long long ldx, __nv_bfloat16 *out, int ldo, int planes) {
+mx_planes8_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols, long long ldx, uint8_t *out, int ldo, int Mc, int planes,
+                  int *flags, int n_flags) {
   pdl_launch_dependents();   // (the product waits for this kernel's end before it reads activations)
-  const Placer pl(ldo / 8);
-  const float top = __uint_as_float(0x7f7f0000u);
-#pragma unroll
-  for (int i = 0; i < kConvUnroll; ++i) {
-    const Place at = pl.at(i * kConvThreads + threadIdx.x);
-    if (at.row >= rows) continue;
-    float v[8];
-    load8<TYPE, VEC>(x + at.row * ldx, at.col, cols, v);
-    for (int p = 0; p < planes; ++p) {
-      __align__(16) uint16_t h[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool fin = (__float_as_uint(v[j]) & 0x7f800000u) != 0x7f800000u;
-        const __nv_bfloat16 b = __float2bfloat16_rn(fin ? fminf(fmaxf(v[j], -top), top) : v[j]);
-        h[j] = __bfloat16_as_ushort(b);
-        v[j] = fin ? v[j] - __bfloat162float(b) : 0.f;
-      }
-      *reinterpret_cast<uint4 *>(out + ((size_t)p * rows + at.row) * ldo + at.col) = *reinterpret_cast<const uint4 *>(h);
-    }
-  }
+  pdl_wait();                // (x may come from the kernel before, whose activations may be in the same workspace)
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < n_flags; i += kConvThreads) flags[i] = 0;
+  const long long i = (long long)blockIdx.x * kConvThreads + threadIdx.x;
+  const int per = ldo / 8;
+  const long long row = i / per;
+  const int col = (int)(i - row * per) * 8;
+  float v[8];
+  mx_load8<TYPE>(x + row * ldx, row < rows, col, cols, VEC, v);
+  const int z = (int)(row / Mc), m = (int)(row - (long long)z * Mc), ncols = planes * Mc;
+  mx_to_planes(v, row < rows, out + ((size_t)z * (ldo >> 7) + (col >> 7)) * mx_x_block(ncols), ncols * kMxTileK, Mc, planes, m, col & 127);
 }
 
 bool aligned(const void *p, long long ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
@@ -237,7 +188,7 @@ cudaError_t launch_mx_quantise(const void *x, int type, int rows, int cols, long
   const int nb = (cols + kMxBlock - 1) / kMxBlock;
   if (rows <= 0 || cols <= 0) return cudaSuccess;
   const bool vec = aligned(x, ldx, type == MX_F32 ? 4 : 2);
-#define F(T, V) mx_quantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const Elem<T>::raw *)x, rows, cols, ldx, nb, (uint32_t *)codes, scales)
+#define F(T, V) mx_quantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const MxElem<T>::raw *)x, rows, cols, ldx, nb, (uint32_t *)codes, scales)
   MX_BY_TYPE(type, vec, F)
 #undef F
   return cudaGetLastError();
@@ -248,7 +199,7 @@ cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, in
   const int nb = (cols + kMxBlock - 1) / kMxBlock;
   if (rows <= 0 || cols <= 0) return cudaSuccess;
   const bool vec = aligned(y, ldy, type == MX_F32 ? 4 : 2);
-#define F(T, V) mx_dequantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const uint32_t *)codes, scales, rows, cols, nb, (Elem<T>::raw *)y, ldy)
+#define F(T, V) mx_dequantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const uint32_t *)codes, scales, rows, cols, nb, (MxElem<T>::raw *)y, ldy)
   MX_BY_TYPE(type, vec, F)
 #undef F
   return cudaGetLastError();
@@ -264,12 +215,28 @@ cudaError_t launch_mx_lay_out(const uint8_t *codes, const uint8_t *scales, int n
   return lay_out(codes, scales, n_rows, n_rows, r0, nb, rm, w, st);
 }
 
-cudaError_t launch_mx_planes(const void *x, int type, int rows, int cols, long long ldx, __nv_bfloat16 *out, int ldo, int planes, cudaStream_t st) {
+template <int TYPE, bool VEC>
+static cudaError_t planes8(const void *x, int rows, int cols, long long ldx, uint8_t *out, int Mc, int planes, int *flags, int n_flags,
+                           cudaStream_t st, bool pdl) {
+  const int ldo = (cols + 127) / 128 * 128;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(((long long)rows * (ldo / 8) + kConvThreads - 1) / kConvThreads));
+  cfg.blockDim = dim3(kConvThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = pdl ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, mx_planes8_kernel<TYPE, VEC>, (const typename MxElem<TYPE>::raw *)x, (long long)rows, cols, ldx, out, ldo, Mc, planes,
+                            flags, n_flags);
+}
+cudaError_t launch_mx_planes8(const void *x, int type, int rows, int cols, long long ldx, uint8_t *out, int Mc, int planes, int *flags, int n_flags,
+                              cudaStream_t st, bool pdl) {
   const bool vec = aligned(x, ldx, type == MX_F32 ? 4 : 2);
-#define F(T, V) mx_planes_kernel<T, V><<<conv_blocks(rows, ldo / 8), kConvThreads, 0, st>>>((const Elem<T>::raw *)x, rows, cols, ldx, out, ldo, planes)
+#define F(T, V) return planes8<T, V>(x, rows, cols, ldx, out, Mc, planes, flags, n_flags, st, pdl)
   MX_BY_TYPE(type, vec, F)
 #undef F
-  return cudaGetLastError();
 }
 
 }  // namespace ts
@@ -340,10 +307,22 @@ ts_status packed_ok(const void *codes, const void *scales, int64_t rows, int64_t
   if ((uintptr_t)codes % 16) return set_error(TS_ERR_ARG, "codes must be 16-byte aligned");
   return TS_OK;
 }
-int planes_of(int32_t type) { return type == TS_MX_BF16 ? 1 : 2; }
-int padded(int64_t k) { return (int)((k + 7) / 8 * 8); }
+int planes_of(int32_t type) { return type == TS_MX_BF16 ? 2 : type == TS_MX_F16 ? 3 : 5; }
 uint64_t tiles_of(int64_t n) { return (uint64_t)(n + ts::kMxTileN - 1) / ts::kMxTileN; }
 uint64_t kblocks_of(int64_t k) { return (uint64_t)(k + ts::kMxTileK - 1) / ts::kMxTileK; }
+
+// What a product keeps in its workspace: the activations' planes, where it is dealt out in runs a flag
+// and a slab of sums for each CTA.
+struct Workspace { uint64_t flags, slabs, bytes; };
+Workspace workspace_of(int64_t k, int planes, const ts::MxPlan &p) {
+  Workspace w;
+  if (p.own) return Workspace{};
+  w.flags = (uint64_t)p.chunks * kblocks_of(k) * ts::mx_x_block(planes * p.Mc);
+  w.slabs = w.flags + (p.stream ? ((uint64_t)p.ctas * 4 + 127) / 128 * 128 : 0);
+  w.bytes = w.slabs + (p.stream ? (uint64_t)p.ctas * p.Mc * ts::kMxTileN * 4 : 0);
+  return w;
+}
+constexpr int kMostSms = 256;   // (the size of a workspace is asked for without a device)
 
 #define MX_TRY(call)                                                                                      \
   do {                                                                                                    \
@@ -391,7 +370,7 @@ ts_status ts_mxfp4_lay_out(const void *codes, const void *scales, int64_t n, int
   MX_OK(matrix_ok(n, k));
   MX_OK(packed_ok(codes, scales, n, k));
   if (!n || !k) return TS_OK;
-  if (!matrix || (uintptr_t)matrix % 16) return set_error(TS_ERR_ARG, "matrix is null or not 16-byte aligned");
+  if (!matrix || (uintptr_t)matrix % 128) return set_error(TS_ERR_ARG, "matrix is null or not 128-byte aligned");
   MxDevice d;
   MX_OK(device_of_call(&d));
   const int tiles = (int)tiles_of(n);
@@ -400,18 +379,55 @@ ts_status ts_mxfp4_lay_out(const void *codes, const void *scales, int64_t n, int
   return TS_OK;
 }
 
+ts_status ts_mxfp4_matrix_init(ts_mxfp4_matrix *m, const void *data, int64_t n, int64_t k) {
+  if (!m) return set_error(TS_ERR_ARG, "null argument");
+  MX_OK(matrix_ok(n, k));
+  std::memset(m, 0, sizeof *m);
+  m->n = n;
+  m->k = k;
+  if (!n || !k) return TS_OK;
+  if (!data || (uintptr_t)data % 128) return set_error(TS_ERR_ARG, "matrix is null or not 128-byte aligned");
+  MxDevice d;
+  MX_OK(device_of_call(&d));
+  CUtensorMap map;
+  static_assert(sizeof map == sizeof m->map, "a descriptor has 128 bytes");
+  const cuuint64_t dims[3] = {128, 128, (cuuint64_t)(tiles_of(n) * kblocks_of(k))};
+  const cuuint64_t strides[2] = {64, ts::kMxTileBytes};
+  const cuuint32_t box[3] = {128, 128, 1}, es[3] = {1, 1, 1};
+  const CUresult r = g_encode.load(std::memory_order_acquire)(&map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 3, const_cast<void *>(data), dims, strides,
+                                                              box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return set_error(TS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  m->data = data;
+  std::memcpy(m->map, &map, sizeof map);
+  return TS_OK;
+}
+
 ts_status ts_mxfp4_product_workspace(int64_t rows, int64_t n, int64_t k, int32_t x_type, uint64_t *bytes) {
   if (!bytes) return set_error(TS_ERR_ARG, "null argument");
   MX_OK(matrix_ok(n, k));
   MX_OK(matrix_ok(rows, k));
   if (!type_ok(x_type)) return set_error(TS_ERR_ARG, "unknown element type %d", x_type);
-  *bytes = (uint64_t)planes_of(x_type) * rows * padded(k) * 2;
+  *bytes = 0;
+  if (rows && n && k) {
+    // Enough for fewer rows too, and whatever the device's number of SMs: as many flags and slabs as there may be, chunks counted at their
+    // largest.
+    const int planes = planes_of(x_type), tiles = (int)tiles_of(n), n_kb = (int)kblocks_of(k);
+    ts::MxPlan p = ts::mx_plan((int)rows, tiles, n_kb, planes, 1);
+    const ts::MxPlan full = ts::mx_plan(1 << 20, 1, 1, planes, 1);
+    if (p.chunks > 1) p.Mc = full.Mc;
+    p.own = false;
+    p.stream = true;
+    p.ctas = 2 * kMostSms;
+    *bytes = workspace_of(k, planes, p).bytes;
+  }
   return TS_OK;
 }
 
 ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
-  if (!a) return set_error(TS_ERR_ARG, "null argument");
-  const int64_t M = a->rows, N = a->n, K = a->k;
+  if (!a || !a->matrix) return set_error(TS_ERR_ARG, "null argument");
+  const ts_mxfp4_matrix *w = a->matrix;
+  const int64_t M = a->rows, N = w->n, K = w->k;
   MX_OK(matrix_ok(N, K));
   MX_OK(matrix_ok(M, K));
   MX_OK(strided_ok("x", a->x, a->x_type, M, K, a->ldx));
@@ -425,23 +441,15 @@ ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
     MX_TRY(cudaMemset2DAsync(a->y, a->ldy * type_size(a->y_type), 0, N * type_size(a->y_type), M, st));
     return TS_OK;
   }
-  if (!a->matrix || (uintptr_t)a->matrix % 16) return set_error(TS_ERR_ARG, "matrix is null or not 16-byte aligned");
+  if (!w->data) return set_error(TS_ERR_ARG, "the matrix has no data");
 
-  // The product reads bf16 planes with 16-byte aligned rows: bf16 rows that are, as they are, all others from the workspace.
   const int planes = planes_of(a->x_type);
-  const bool direct = a->x_type == TS_MX_BF16 && ts::aligned(a->x, a->ldx, 2);
-  void *base = const_cast<void *>(a->x);
-  uint64_t row_bytes = a->ldx * 2;
-  if (!direct) {
-    const uint64_t need = (uint64_t)planes * M * padded(K) * 2;
-    if (!a->workspace || a->workspace_bytes < need || (uintptr_t)a->workspace % 16)
-      return set_error(TS_ERR_ARG, "workspace of %llu bytes, 16-byte aligned, needed for these rows", (unsigned long long)need);
-    MX_TRY(ts::launch_mx_planes(a->x, a->x_type, (int)M, (int)K, a->ldx, (__nv_bfloat16 *)a->workspace, padded(K), planes, st));
-    base = a->workspace;
-    row_bytes = (uint64_t)padded(K) * 2;
-  }
+  const ts::MxPlan p = ts::mx_plan((int)M, (int)tiles_of(N), (int)kblocks_of(K), planes, std::min(d.sms, kMostSms));
+  const Workspace ws = workspace_of(K, planes, p);
+  if (ws.bytes && (!a->workspace || a->workspace_bytes < ws.bytes || (uintptr_t)a->workspace % 128))
+    return set_error(TS_ERR_ARG, "workspace of %llu bytes, 128-byte aligned, needed for these rows", (unsigned long long)ws.bytes);
   ts::MxArgs g{};
-  g.w = (const uint8_t *)a->matrix;
+  g.w = (const uint8_t *)w->data;
   g.N = (int)N; g.M = (int)M;
   g.tiles = (int)tiles_of(N); g.n_kb = (int)kblocks_of(K);
   g.planes = planes;
@@ -449,19 +457,17 @@ ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
   g.y = a->y; g.ldy = a->ldy; g.y_type = a->y_type;
   const size_t ysz = type_size(a->y_type);
   g.vec = a->ldy % 4 == 0 && (uintptr_t)a->y % (4 * ysz) == 0;
-  const ts::MxPlan p = ts::mx_plan((int)M, g.tiles, g.n_kb, planes, d.sms);
-  g.Mc = p.Mc;
-  CUtensorMap map;
-  {
-    const cuuint64_t dims[3] = {(cuuint64_t)K, (cuuint64_t)M, (cuuint64_t)planes};
-    const cuuint64_t strides[2] = {row_bytes, row_bytes * (cuuint64_t)M};
-    const cuuint32_t box[3] = {64, (cuuint32_t)g.Mc, (cuuint32_t)planes}, es[3] = {1, 1, 1};
-    const CUresult r = g_encode.load(std::memory_order_acquire)(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, es,
-                                                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return set_error(TS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
-  }
-  MX_TRY(ts::launch_mx_product(ts::MX_STORE, map, g, p.tiles_per_cta, p.cluster, st, true));
+  uint8_t *base = (uint8_t *)a->workspace;
+  g.x = p.own ? a->x : base;
+  g.ldx = a->ldx; g.x_type = a->x_type; g.K = (int)K;
+  g.vec_x = ts::aligned(a->x, a->ldx, (int)type_size(a->x_type));
+  g.flags = (int *)(base + ws.flags);
+  g.slabs = (float *)(base + ws.slabs);
+  if (!p.own)
+    MX_TRY(ts::launch_mx_planes8(a->x, a->x_type, (int)M, (int)K, a->ldx, base, p.Mc, planes, g.flags, p.stream ? p.ctas : 0, st, true));
+  CUtensorMap tw;
+  std::memcpy(&tw, w->map, sizeof tw);
+  MX_TRY(ts::launch_mx_product(ts::MX_STORE, tw, g, p, st, true));
   return TS_OK;
 }
 

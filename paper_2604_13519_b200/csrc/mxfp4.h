@@ -11,35 +11,27 @@ constexpr int kMxTileN = 128;         // weight rows of a stored block
 constexpr int kMxCodeBytes = kMxTileN * kMxTileK / 2;
 constexpr int kMxTileBytes = kMxCodeBytes + kMxTileN * (kMxTileK / kMxBlock);   // codes, then scales: 8704
 
-// A laid-out matrix of N x K: ceil(N / 128) x ceil(K / 128) blocks, k-block major (as the bf16 matrices are, see w_block).  Inside a
-// block: codes [4 MX blocks][128 rows][16 bytes], scales [128 rows][4 MX blocks].
-//
-// The 32 codes of a row and MX block are four words of eight, in the order in which a thread takes them apart (mx_unpack): the low
-// half of word i holds elements 8i, 8i + 2, 8i + 4, 8i + 6, the high half those after them, each half with the bits of its four
-// elements at
-//     element 0: sign 15, code 8..6    1: sign 12, code 5..3    2: sign 9, code 2..0    3: sign 14, code bits 13, 11, 10
-// so that three of the four pairs come out as bf16 (sign at 15, the code's exponent and mantissa bits at 8..6) with one shift and one
-// mask for both halves, and the fourth with three of each: 11 logical instructions and four multiplications for eight weights.
-// Nibbles in their plain order take 16.
-__host__ __device__ inline uint32_t mx_place(uint32_t nib, int j) {   // the 16-bit half's bits of element j
-  const uint32_t s = nib >> 3, c = nib & 7;
-  switch (j) {
-    case 0: return s << 15 | c << 6;
-    case 1: return s << 12 | c << 3;
-    case 2: return s << 9 | c;
-    default: return s << 14 | (c >> 2) << 13 | (c & 3) << 10;
-  }
-}
+// A laid-out matrix of N x K: ceil(N / 128) x ceil(K / 128) blocks, a tile's blocks one after the other.  Inside a block: elements [128 rows][64 bytes], the even one of two in the low half of a byte, then scales [32][4][4]: bytes of row 32 j + l at
+// [l][j], one per MX block (the order in which tcgen05.cp takes them to tensor memory).
+__host__ __device__ inline int mx_scale_at(int row) { return kMxCodeBytes + (row & 31) * 16 + (row >> 5) * 4; }
+
+__host__ __device__ inline int mx_block(int tile, int kb, int n_kb) { return tile * n_kb + kb; }
 
 enum : int { MX_BF16 = 0, MX_F16 = 1, MX_F32 = 2 };   // element types of activations and results (TS_MX_*)
 
 struct MxArgs {
-  const uint8_t *w;       // laid-out matrix
-  int N, M;               // features, activation rows
-  int tiles, n_kb;        // 128-row tiles and 128-column blocks of the matrix
-  int Mc, planes;         // activation rows per CTA (a multiple of 8, planes x Mc one of 16), bf16 planes that are added
-  int stages;             // filled in by the launcher
-  int *err;               // device status word (null: not wanted)
+  const uint8_t *w;          // laid-out matrix
+  const void *x;             // the activations' planes, see launch_mx_planes8; with plan.own the rows themselves:
+  long long ldx;             // row stride
+  int x_type, vec_x, K;      // type, rows can be read 16 bytes at a time, columns
+  float *slabs;              // [CTA][Mc][128] sums of tiles that the CTA has without their last k-blocks
+  int *flags;                // [CTA] its slab is there (zero before the launch)
+  int N, M;                  // features, activation rows
+  int tiles, n_kb;           // 128-row tiles and 128-column blocks of the matrix
+  int planes;                // planes of e4m3 numbers that are added
+  int Mc, chunks, stages, n_acc;   // filled in by the launcher: activation rows per tile of the result, their chunks, stages of the ring, accumulators
+  long long units;           // tiles x chunks x k-blocks
+  int *err;                  // device status word (null: not wanted)
   unsigned long long *stamp;
   // MX_STORE
   void *y;
@@ -54,13 +46,147 @@ struct MxArgs {
 };
 enum : int { MX_STORE = 0, MX_SWIGLU = 1, MX_LOGITS = 2 };   // what a product does with its sums
 
-// How a product is dealt out.
-struct MxPlan { int Mc, tiles_per_cta, cluster; };
-MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms);
+#ifdef __CUDACC__
+template <int TYPE> struct MxElem;
+template <> struct MxElem<MX_BF16> { typedef uint16_t raw; };
+template <> struct MxElem<MX_F16> { typedef uint16_t raw; };
+template <> struct MxElem<MX_F32> { typedef uint32_t raw; };
+template <int TYPE> __device__ __forceinline__ float mx_to_f32(typename MxElem<TYPE>::raw r) {
+  if constexpr (TYPE == MX_BF16) return __uint_as_float((uint32_t)r << 16);
+  else if constexpr (TYPE == MX_F16) return __half2float(__ushort_as_half(r));
+  else return __uint_as_float(r);
+}
+template <int TYPE> __device__ __forceinline__ typename MxElem<TYPE>::raw mx_from_f32(float v) {
+  if constexpr (TYPE == MX_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+  else if constexpr (TYPE == MX_F16) return __half_as_ushort(__float2half_rn(v));
+  else return __float_as_uint(v);
+}
 
-// `ta`: bf16 activations [planes][rows][K], box {64, Mc, planes}, 128-byte swizzle.  cluster: CTAs along K that complete a tile's
-// sums together.  tiles_per_cta: 1 or 2 weight tiles.
-cudaError_t launch_mx_product(int epi, const CUtensorMap &ta, MxArgs g, int tiles_per_cta, int cluster, cudaStream_t st, bool pdl);
+// elements [c, c + 8) of a row of `cols` as they are, zeros behind its end and where `there` is false
+template <int TYPE> struct MxRaw8 { __align__(16) typename MxElem<TYPE>::raw r[8]; };
+template <int TYPE>
+__device__ __forceinline__ void mx_fetch8(const typename MxElem<TYPE>::raw *p, bool there, int c, int cols, bool vec, MxRaw8<TYPE> &x) {
+  if (vec && there && c + 8 <= cols) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(x.r[0]) / 2; ++i) reinterpret_cast<uint4 *>(x.r)[i] = __ldg(reinterpret_cast<const uint4 *>(p + c) + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.r[i] = there && c + i < cols ? p[c + i] : 0;
+  }
+}
+template <int TYPE> __device__ __forceinline__ void mx_widen8(const MxRaw8<TYPE> &x, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = mx_to_f32<TYPE>(x.r[i]);
+}
+template <int TYPE>
+__device__ __forceinline__ void mx_load8(const typename MxElem<TYPE>::raw *p, bool there, int c, int cols, bool vec, float (&v)[8]) {
+  MxRaw8<TYPE> x;
+  mx_fetch8<TYPE>(p, there, c, cols, vec, x);
+  mx_widen8<TYPE>(x, v);
+}
+
+// Eight elements at columns col .. col + 7 of row m (m: within its chunk) into the planes of a block of 128 columns (col: within it) at
+// `blk`; its scales lie `act_bytes` further on.  Four neighbouring threads share an MX block.
+//
+// x as planes of e4m3 numbers (four significant bits each).  A block's first scale puts its largest magnitude into [2^7, 2^8), so that
+// it and what rounding leaves of it, at most 2^3, stay in range (448); the next plane holds sixteen times the remainder with a scale
+// of a sixteenth, and so on.  With two planes all bf16 numbers down to 2^-14 of the block's largest come out exactly (eight bits), and
+// what is lost of smaller ones is below 2^-21 of it; three planes do the same for fp16 (eleven bits).  Each remainder is exact in
+// fp32.  A block with an infinity or NaN gets the scale byte 255, which makes its products NaN.
+__device__ __forceinline__ void mx_to_planes(float (&v)[8], bool there, uint8_t *blk, int act_bytes, int Mc, int planes, int m, int col) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  if (!there) return;
+  const uint32_t e = top >> 23;
+  uint32_t s = e > 7u ? e - 7u : 0u;
+  const float f = e == 255u ? 0.f : __uint_as_float((254u - s) << 23);   // 2^(127 - s)
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = e == 255u ? 0.f : v[j] * f;
+  uint8_t *sc = blk + act_bytes + (col >> 5);
+  for (int p = 0; p < planes; ++p) {
+    uint32_t q[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint16_t a, b;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(a) : "f"(v[4 * h + 1]), "f"(v[4 * h]));
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(v[4 * h + 3]), "f"(v[4 * h + 2]));
+      q[h] = a | (uint32_t)b << 16;
+      uint32_t ha, hb;
+      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(ha) : "h"(a));
+      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hb) : "h"(b));
+      const float2 fa = __half22float2(*reinterpret_cast<const __half2 *>(&ha)), fb = __half22float2(*reinterpret_cast<const __half2 *>(&hb));
+      v[4 * h] -= fa.x; v[4 * h + 1] -= fa.y; v[4 * h + 2] -= fb.x; v[4 * h + 3] -= fb.y;
+    }
+    const int c = p * Mc + m;
+    *reinterpret_cast<uint2 *>(blk + c * kMxTileK + (((col >> 4) ^ (c & 7)) << 4) + (col & 8)) = make_uint2(q[0], q[1]);
+    if ((threadIdx.x & 3) == 0) sc[(c >> 7) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4] = (uint8_t)(e == 255u ? 255u : s);
+    const uint32_t next = s > 4u ? s - 4u : 0u;
+    const float up = __uint_as_float((127u + s - next) << 23);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= up;
+    s = next;
+  }
+}
+
+// What becomes of four finished sums: row mg, features n .. n + 3 (a warp's lanes hold 128 consecutive ones)
+template <int EPI> __device__ __forceinline__ void mx_finish(const MxArgs &g, long long mg, int n, const float (&v)[4], int lane) {
+          if constexpr (EPI == MX_STORE) {
+            if (g.y_type == MX_F32) {
+              float *d = (float *)g.y + mg * g.ldy + n;
+              if (g.vec && n + 4 <= g.N) {
+                *reinterpret_cast<float4 *>(d) = make_float4(v[0], v[1], v[2], v[3]);
+              } else {
+                for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = v[j];
+              }
+            } else {
+              uint16_t h[4];
+              for (int j = 0; j < 4; ++j)
+                h[j] = g.y_type == MX_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v[j])) : __half_as_ushort(__float2half_rn(v[j]));
+              uint16_t *d = (uint16_t *)g.y + mg * g.ldy + n;
+              if (g.vec && n + 4 <= g.N) {
+                *reinterpret_cast<uint2 *>(d) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+              } else {
+                for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = h[j];
+              }
+            }
+          } else if constexpr (EPI == MX_LOGITS) {
+            *reinterpret_cast<float4 *>(g.out + (size_t)mg * g.N + n) = make_float4(v[0], v[1], v[2], v[3]);
+            // order-preserving map of the float to an unsigned word; ties resolve to the lowest id (lowest lane, then
+            // lowest of its four)
+            uint32_t best = 0;
+            int bi = 0;
+  #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t u = __float_as_uint(v[j]);
+              u = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+              if (u > best) { best = u; bi = j; }
+            }
+            const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+            if (lane == __ffs(__ballot_sync(0xffffffffu, best == top)) - 1)
+              atomicMax(g.amax + (size_t)mg * kAmaxStride, ((unsigned long long)top << 32) | (unsigned long long)(0xFFFFFFFFu - (uint32_t)(n + bi)));
+          } else {  // MX_SWIGLU: even feature row = gate_f, odd = up_f, f = n / 2
+            __nv_bfloat16 h0, l0, h1, l1;
+            split_bf16(v[0] / (1.f + __expf(-v[0])) * v[1], h0, l0);
+            split_bf16(v[2] / (1.f + __expf(-v[2])) * v[3], h1, l1);
+            const int F = g.N >> 1, f = n >> 1;
+            *reinterpret_cast<__nv_bfloat162 *>(g.act_out + (size_t)mg * F + f) = __halves2bfloat162(h0, h1);
+            if (g.out_planes == 2)
+              *reinterpret_cast<__nv_bfloat162 *>(g.act_out + ((size_t)g.act_rows + mg) * F + f) = __halves2bfloat162(l0, l1);
+          }
+}
+#endif
+
+// How a product is dealt out: activation rows per chunk (a multiple of 8, planes x rows one of 16), chunks; runs of k-blocks (stream) or
+// a tile to each of `ctas` clusters; whether it makes the planes itself.
+struct MxPlan { int Mc, chunks, ctas, cluster; bool stream, own; };
+MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms);
+// `tw`: the matrix's elements, blocks of 128 x 128, widened to bytes by the copy, 128-byte swizzle.
+cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxPlan &p, cudaStream_t st, bool pdl);
+// bytes of 128 columns of the activations with `ncols` = planes x Mc instruction columns: elements, then scales
+__host__ __device__ inline int mx_x_block(int ncols) { return ncols * kMxTileK + 512 * ((ncols + 127) / 128); }
 
 cudaError_t launch_mx_quantise(const void *x, int type, int rows, int cols, long long ldx, uint8_t *codes, uint8_t *scales, cudaStream_t st);
 cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, int rows, int cols, void *y, int type, long long ldy,
@@ -68,7 +194,11 @@ cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, in
 // Rows [r0, r0 + n_rows) of a quantised matrix with nb MX blocks a row (codes, scales: the first of these rows) into the blocks of
 // the laid-out matrix (rm as for launch_retile).
 cudaError_t launch_mx_lay_out(const uint8_t *codes, const uint8_t *scales, int n_rows, int r0, int nb, RowMap rm, uint8_t *w, cudaStream_t st);
-// x [rows][cols] (row stride ldx) as bf16 planes whose sum is x: out [planes][rows][ldo]
-cudaError_t launch_mx_planes(const void *x, int type, int rows, int cols, long long ldx, __nv_bfloat16 *out, int ldo, int planes, cudaStream_t st);
+// x [rows][cols] (row stride ldx) as planes of e4m3 numbers, in blocks as the product's shared memory holds them: [chunk of Mc rows]
+// [128 columns] { elements [column c of the instruction = plane * Mc + row][128 bytes, 16-byte pieces swizzled: piece ^ (c & 7)],
+// scales [c / 128][lane c % 32][word c / 32 % 4][4 bytes, one per MX block] }.  Rows behind the last one of a chunk stay as they are.
+// Clears n_flags words at `flags`.
+cudaError_t launch_mx_planes8(const void *x, int type, int rows, int cols, long long ldx, uint8_t *out, int Mc, int planes, int *flags, int n_flags,
+                              cudaStream_t st, bool pdl);
 
 }  // namespace ts

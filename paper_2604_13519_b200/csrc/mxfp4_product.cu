@@ -1,13 +1,32 @@
-// y[m][n] = sum_k x[m][k] * W[n][k] with W in MXFP4 and the activations as bf16 planes (their sum is x; one plane for bf16 rows).
+// y[m][n] = sum_k x[m][k] * W[n][k] with W in MXFP4.  The block-scaled form of the tensor cores' instruction (kind::mxf8f6f4) takes the
+// weights' four-bit elements and scale bytes as they are, so a CTA only moves them.  (Widening them to bf16 in registers on the
+// way into tensor memory, the first form of this kernel, took 1600 warp instructions for a block of 128 x 128 elements, more than
+// the SM issues in the block's share of the memory's time: LM head of 151936 x 4096 at 32 rows 92 us.)
 //
-// The tensor cores multiply bf16: every e2m1 value times a power of two is a bf16 number, so products are exact and sums are
-// fp32, as with bf16 weights.  What the four bits save is memory traffic: 17 bytes for 32 weights instead of 64.  The weights are
-// widened on their way: threads take a row's 32 codes of a block out of shared memory, turn them into bf16 in registers and put
-// them into TENSOR memory, where the product reads its 128-row operand from (lane = weight row, two elements per column).  So the
-// widened weights never pass through shared memory, whose bandwidth they would take twice (written, and read by the product).
+// The instruction's other operand has eight bits at most: the activations come as planes of e4m3 numbers with a scale byte per 32
+// columns and plane, each plane holding what the ones before it left over (mx_planes8_kernel).  Planes are stacked along the
+// instruction's N dimension, as the bf16 planes of gemm_tcgen05.cu are, and the epilogue adds their columns.
 //
-// Roles: warp 0 brings in weight blocks (bulk copies: a block is contiguous) and activation boxes (TMA), warp 1 allocates tensor
-// memory and issues the products, the others (four per weight tile) widen and at the end take the sums out.
+// Shared memory holds a block's elements in eight-bit containers: TMA puts them there from packed memory (16U4_ALIGN16B).  Scales go from
+// shared into tensor memory (tcgen05.cp: 32 lanes x 16 bytes, repeated in all four lane quarters): word j of lane l = the four scales
+// of row 32 j + l along a block's 128 columns.
+//
+// Two ways to deal the work out; which one a product takes depends on its tiles alone (128 features x a chunk of rows).
+//
+// kStream, for more tiles than CTAs fit: in k-blocks.  (tile, k-block) pairs in order, an equal run of them to each of two CTAs per SM, so
+// that all SMs stream the same bytes whatever the matrix's shape and a launch has one start and one end.  A CTA walks its run from the
+// end to the start.  A tile that it has without its last k-block (the first that it walks) it leaves as partial sums for the CTAs
+// behind it; a tile that it has without its first k-block (its last) it finishes, adding the partial sums of the CTAs before it, in
+// order of k.  Those were written at the start of their runs, so there is hardly a wait, and no CTA ever waits for one behind it.
+// Two accumulators where the tensor memory holds them: the epilogue of one tile runs under the products of the next.
+//
+// Otherwise one tile to a CTA, or, where that leaves places empty, to a cluster of CTAs along K, whose sums meet through
+// distributed shared memory: less of an exchange than through L2, which counts where a CTA has few k-blocks.
+//
+// Up to two rows the CTAs of the second kind make the planes themselves (kOwn): four more warps turn a stage's 128 columns into e4m3
+// on the way into shared memory, which saves a launch; for more rows a kernel ahead does it once for all CTAs (launch_mx_planes8).
+//
+// Roles: warp 0 = copies, warp 1 = tensor memory, scales and products, warps 2..5 = epilogue, warps 6..9 = planes (kOwn).
 // Every wait is bounded; on expiry the CTA records an error word and leaves through the normal exit.
 #include <cuda_fp16.h>
 
@@ -17,79 +36,140 @@
 
 namespace ts {
 
-static constexpr int kMxMaxStages = 12;
-static constexpr int kMxWide = 2;          // widened blocks in tensor memory: one being multiplied while the next is written
-static constexpr int kWideCols = kMxTileK / 2;
+static constexpr int kProdMaxStages = 12;
+static constexpr int kProdW = kMxTileN * kMxTileK;   // a block's elements in shared memory
+static constexpr int kProdStaging = 2 * 8 * kMxTileN * 4;   // eight rows of sums, twice
+static constexpr int kProdAcc = 224;                  // most columns of an accumulator: with 24 of scales (two stages) half of the tensor memory
+static constexpr int kProdCtas = 2;                   // per SM
 
-struct __align__(16) MxSmemCtl {
-  uint64_t full[kMxMaxStages];
-  uint64_t empty[kMxMaxStages];
-  uint64_t wide_full[kMxWide];
-  uint64_t wide_empty[kMxWide];
-  uint64_t tmem_full;
+struct __align__(16) ProdSmemCtl {
+  uint64_t full[kProdMaxStages];
+  uint64_t empty[kProdMaxStages];
+  uint64_t acc_full[2];
+  uint64_t acc_empty[2];
   uint32_t tmem_base;
   uint32_t abort_flag;
 };
 
-__device__ __forceinline__ void mx_error(const MxArgs &g, int code) { if (g.err) atomicExch(g.err, code); }
+__device__ __forceinline__ void prod_error(const MxArgs &g, int code) { if (g.err) atomicExch(g.err, code); }
 
-__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
+// D[tmem] (+)= (A x scales) * (B x scales), A e2m1 and B e4m3 in shared memory, K = 32
+__device__ __forceinline__ void umma_mx(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+      : "memory");
+}
+// Instruction descriptor: A e2m1, B e4m3, both K-major, scales ue8m0, D fp32, M x N; the scales' byte within their words is added (see
+// mx_scale_byte)
+__device__ __forceinline__ uint32_t umma_idesc_mx(uint32_t M, uint32_t N) {
+  return (5u << 7) | (0u << 10) | ((N >> 3) << 17) | (1u << 23) | ((M >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t i) { return (i << 4) | (i << 29); }
+
+// 32 x 16 bytes of shared memory -> four columns of all four lane quarters
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// no swizzle, 8 rows x 16 bytes contiguous, the next 8 rows 128 bytes further on
+__device__ __forceinline__ uint64_t scales_desc(uint32_t saddr) {
+  return (uint64_t)((saddr >> 4) & 0x3FFF) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
-// Eight codes (see mx_place) -> four bf16 pairs.  The masked bits read as bf16 are value x 2^-126 (subnormal for 0.5), which the
-// multiplication by 2^(s - 1) brings to value x 2^(s - 127) without rounding.
-__device__ __forceinline__ void mx_unpack(uint32_t w, uint32_t mul, uint32_t *r) {
-  constexpr uint32_t M = 0x81C081C0u;
-  r[0] = bf16x2_mul(w & M, mul);
-  r[1] = bf16x2_mul((w << 3) & M, mul);
-  r[2] = bf16x2_mul((w << 6) & M, mul);
-  uint32_t t = (w >> 4) & 0x00C000C0u;
-  t |= (w >> 5) & 0x01000100u;
-  t |= (w << 1) & 0x80008000u;
-  r[3] = bf16x2_mul(t, mul);
+// The run of CTA c out of G in units (tile x chunk) * n_kb + k-block
+__device__ __forceinline__ long long prod_start(const MxArgs &g, int c, int G) { return (long long)c * g.units / G; }
+
+// One tile of a run: item = tile * chunks + chunk, k-blocks [kb0, kb1)
+struct ProdSeg {
+  int item, kb0, kb1;
+};
+// the segment that ends at unit `hi` of a run that starts at `lo`
+__device__ __forceinline__ ProdSeg prod_seg(const MxArgs &g, long long lo, long long hi) {
+  ProdSeg t;
+  t.item = (int)((hi - 1) / g.n_kb);
+  const long long first = (long long)t.item * g.n_kb;
+  t.kb0 = (int)(max(lo, first) - first);
+  t.kb1 = (int)(hi - first);
+  return t;
 }
 
-// Scale byte -> multiplier pairs: 2^(s - 1) while that is a bf16 number (s <= 128), else 2^127 and a second factor.
-__device__ __forceinline__ uint32_t mx_factor(uint32_t s) {
-  const uint32_t b = (min(s, 128u) + 126u) << 7;
-  return b | b << 16;
+__device__ __forceinline__ int ld_acquire(const int *p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
 }
-__device__ __forceinline__ uint32_t mx_factor2(uint32_t s) {   // (255: not a number)
-  const uint32_t b = s == 255u ? 0x7FC0u : (s > 128u ? (s - 1u) << 7 : 0x3F80u);
-  return b | b << 16;
+// until the flag is set, or about two seconds
+__device__ __forceinline__ bool wait_flag(const int *p) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 0;; ++it) {
+    if (ld_acquire(p)) return true;
+    if ((it & 63u) == 63u) {
+      const uint64_t now = global_timer_ns();
+      if (t0 == 0) t0 = now;
+      else if (now - t0 > 2000000000ull) return false;
+    }
+  }
 }
 
-template <int WT, int EPI>
-__global__ void __launch_bounds__(64 + 128 * WT, WT == 1 ? 2 : 1)
-mx_product_kernel(const __grid_constant__ CUtensorMap tmap_a, const MxArgs g) {
+// A block's scales into tensor memory (at `sf`) and its products.  A copy waits for nothing that was issued before it, so a stage of the
+// ring has columns of its own for its scales: by the time that its barrier says full again, the products that read them are done.
+__device__ __forceinline__ void prod_block(uint32_t sa, uint32_t sf, uint32_t d, uint32_t idesc, int act_bytes, int sb_words, bool accumulate) {
+  const uint32_t sx = sa + kProdW, sfx = sx + act_bytes, sfw = sfx + 512 * sb_words;
+  tmem_cp_scales(sf, scales_desc(sfw));
+  tmem_cp_scales(sf + 4, scales_desc(sfx));
+  if (sb_words > 1) tmem_cp_scales(sf + 8, scales_desc(sfx + 512));
+  const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sx);
+#pragma unroll
+  for (int kk = 0; kk < kMxTileK / 32; ++kk)   // 32 elements along K are 32 bytes of a row
+    umma_mx(d, da + 2 * kk, db + 2 * kk, idesc | mx_scale_byte(kk), sf, sf + 4, accumulate || kk != 0);
+}
+
+// eight rows' sums of this thread's feature, planes added
+__device__ __forceinline__ void prod_sums(const MxArgs &g, uint32_t taddr, float (&v)[8]) {
+  uint32_t r[8];
+  tmem_ld8(taddr, r);
+  tmem_wait_ld();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+  for (int p = 1; p < g.planes; ++p) {
+    tmem_ld8(taddr + p * g.Mc, r);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(r[i]);
+  }
+}
+
+template <int EPI, bool kStream, bool kOwn, int TYPE>
+__global__ void __launch_bounds__(kOwn ? 320 : 192, kProdCtas)
+mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  const int box_bytes = g.planes * g.Mc * 128;                       // 64 columns of the activations
-  const int act_bytes = 2 * box_bytes;
-  const int stage_bytes = (act_bytes + WT * kMxTileBytes + 1023) & ~1023;
-  MxSmemCtl *ctl = reinterpret_cast<MxSmemCtl *>(smem + (size_t)g.stages * stage_bytes);
+  const int ncols = g.planes * g.Mc, sb_words = (ncols + 127) / 128;   // (512 bytes of scales for 128 columns)
+  const int act_bytes = ncols * kMxTileK, scale_bytes = 512 * (1 + sb_words);
+  const int stage_bytes = kProdW + ((act_bytes + scale_bytes + 1023) & ~1023);
+  uint8_t *staging = smem + (size_t)g.stages * stage_bytes;
+  ProdSmemCtl *ctl = reinterpret_cast<ProdSmemCtl *>(staging + kProdStaging);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tile0 = blockIdx.x * WT, nt = min(WT, g.tiles - tile0);   // weight tiles of this CTA (the last may have one of two)
-  const int split = blockIdx.y, C = (int)gridDim.y;                   // the CTA's rank in its cluster, which spans the K slices
-  const int m0 = blockIdx.z * g.Mc, M = min(g.Mc, g.M - m0);          // its activation rows
-  const int kb0 = (int)(((long long)split * g.n_kb) / C), nkb = (int)(((long long)(split + 1) * g.n_kb) / C) - kb0;
-  const uint32_t ncols = g.planes * g.Mc, acc_cols = (ncols + 31) & ~31u;
-  uint32_t alloc_cols = 32;
-  while (alloc_cols < WT * (acc_cols + kMxWide * kWideCols)) alloc_cols <<= 1;
+  const int cta = blockIdx.x, G = gridDim.x;
+  const int split = blockIdx.y, C = kStream ? 1 : (int)gridDim.y;   // the CTA's rank in its cluster, which spans the K slices of a tile
+  const long long first = (long long)cta * g.n_kb;   // (one tile: cta is the item)
+  const long long u0 = kStream ? prod_start(g, cta, G) : first + (long long)split * g.n_kb / C;
+  const long long u1 = kStream ? prod_start(g, cta + 1, G) : first + (long long)(split + 1) * g.n_kb / C;
+  const uint32_t acc_cols = (ncols + 31) & ~31u, n_acc = g.n_acc, scales_at = n_acc * acc_cols, set_cols = 4 + 4 * sb_words;
+  uint32_t alloc_cols = 64;
+  while (alloc_cols < scales_at + g.stages * set_cols) alloc_cols <<= 1;
 
   if (warp == 0 && lane == 0) {
-    tma_prefetch_desc(&tmap_a);
+    tma_prefetch_desc(&tmap_w);
     for (int s = 0; s < g.stages; ++s) {
-      mbar_init(smem_u32(&ctl->full[s]), 1);
-      mbar_init(smem_u32(&ctl->empty[s]), 4 * WT + 1);   // the widening warps have the codes, the products have the activations
+      mbar_init(smem_u32(&ctl->full[s]), kOwn ? 2 : 1);   // the copies (and a warp of planes)
+      mbar_init(smem_u32(&ctl->empty[s]), 1);
     }
-    for (int s = 0; s < kMxWide; ++s) {
-      mbar_init(smem_u32(&ctl->wide_full[s]), 4 * WT);
-      mbar_init(smem_u32(&ctl->wide_empty[s]), 1);
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&ctl->acc_full[b]), 1);
+      mbar_init(smem_u32(&ctl->acc_empty[b]), 4);
     }
-    mbar_init(smem_u32(&ctl->tmem_full), 1);
     ctl->abort_flag = 0;
     fence_barrier_init();
   }
@@ -100,249 +180,282 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_a, const MxArgs g) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_base = ctl->tmem_base, wide_base = tmem_base + WT * acc_cols;
+  const uint32_t tmem_base = ctl->tmem_base, scales = tmem_base + scales_at;
   if (threadIdx.x == 0) stamp_min(g.stamp);
   // (placed after this CTA holds its resources, so a waiting dependent can never starve an earlier kernel)
   pdl_launch_dependents();
 
   if (warp == 0) {
-    // ------------------------------------------------------------------ producer
-    if (lane == 0) {
-      const uint64_t pol_w = policy_evict_first(), pol_a = policy_evict_last();
-      const uint32_t w_bytes = nt * kMxTileBytes;
-      auto load_w = [&](int s, int kb) {
-        const uint32_t bar = smem_u32(&ctl->full[s]);
-        mbar_expect_tx(bar, w_bytes + act_bytes);
-        bulk_load(smem_u32(smem + (size_t)s * stage_bytes + act_bytes), g.w + ((size_t)kb * g.tiles + tile0) * kMxTileBytes, w_bytes, bar, pol_w);
-      };
-      auto load_a = [&](int s, int kb) {
-        const uint32_t bar = smem_u32(&ctl->full[s]), dst = smem_u32(smem + (size_t)s * stage_bytes);
-        tma_load_3d(dst, &tmap_a, kb * kMxTileK, m0, 0, bar, pol_a);
-        tma_load_3d(dst + box_bytes, &tmap_a, kb * kMxTileK + 64, m0, 0, bar, pol_a);
-      };
-      // weights do not depend on the previous kernel: they are on their way before the programmatic-dependency wait
-      const int pre = min(g.stages, nkb);
-      for (int it = 0; it < pre; ++it) load_w(it, kb0 + it);
-      pdl_wait();
-      stamp_waited(g.stamp);
-      for (int it = 0; it < pre; ++it) load_a(it, kb0 + it);
-      int s = pre == g.stages ? 0 : pre, it = pre;
-      uint32_t ph = pre == g.stages ? 1 : 0;
-      for (; it < nkb; ++it) {
-        if (!mbar_wait(smem_u32(&ctl->empty[s]), ph ^ 1)) {
-          mx_error(g, DEV_TIMEOUT_EMPTY);
-          break;
+    // ------------------------------------------------------------------ copies
+    // The whole warp walks the loop; one elected lane issues a stage's copies (from a lane in a branch of its own each takes twice as
+    // long, and this warp's time per stage is what bounds a CTA).
+    const uint64_t pol_w = policy_evict_first(), pol_a = policy_evict_last();
+    const int n = (int)(u1 - u0), x_block = act_bytes + 512 * sb_words;
+    auto load_w = [&](uint32_t dst, uint32_t bar, int blk) {
+      mbar_expect_tx(bar, kMxCodeBytes + (kOwn ? 512 : act_bytes + scale_bytes));   // (a copy that widens counts the bytes it reads)
+      tma_load_3d(dst, &tmap_w, 0, 0, blk, bar, pol_w);
+      bulk_load(dst + kProdW + x_block, g.w + (size_t)blk * kMxTileBytes + kMxCodeBytes, 512, bar, pol_w);
+    };
+    auto load_x = [&](uint32_t dst, uint32_t bar, int blk) { bulk_load(dst + kProdW, (const uint8_t *)g.x + (size_t)blk * x_block, x_block, bar, pol_a); };
+    // weights do not depend on the previous kernel: they are on their way before the programmatic-dependency wait
+    const int pre = min(g.stages, n);
+    for (int pass = 0; pass < 2; ++pass) {
+      long long hi = u1;
+      for (int i = 0; i < pre;) {
+        const ProdSeg t = prod_seg(g, u0, hi);
+        const int tile = t.item / g.chunks, z = t.item - tile * g.chunks;
+        for (int kb = t.kb0; kb < t.kb1 && i < pre; ++kb, ++i) {
+          const uint32_t dst = smem_u32(smem) + i * stage_bytes, bar = smem_u32(&ctl->full[i]);
+          if (elect_one()) {
+            if (pass == 0) load_w(dst, bar, mx_block(tile, kb, g.n_kb));
+            else if (!kOwn) load_x(dst, bar, z * g.n_kb + kb);
+          }
+          __syncwarp();
         }
-        load_w(s, kb0 + it);
-        load_a(s, kb0 + it);
-        if (++s == g.stages) { s = 0; ph ^= 1; }
+        hi -= t.kb1 - t.kb0;
       }
-      // whatever becomes of the other roles, this CTA's shared memory stays until its last copies have arrived
-      for (int i = max(0, it - g.stages); i < it; ++i)
-        if (!mbar_wait(smem_u32(&ctl->full[i % g.stages]), (i / g.stages) & 1)) break;
+      if (pass == 0) {
+        pdl_wait();
+        if (lane == 0) stamp_waited(g.stamp);
+      }
     }
+    int s = 0, it = 0;
+    uint32_t ph = 0, dst = smem_u32(smem);
+    bool ok = true;
+    for (long long hi = u1; ok && hi > u0;) {
+      const ProdSeg t = prod_seg(g, u0, hi);
+      const int tile = t.item / g.chunks, z = t.item - tile * g.chunks;
+      for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
+        if (it >= pre) {
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->empty[s]), ph ^ 1));
+          if (!ok) {
+            if (lane == 0) prod_error(g, DEV_TIMEOUT_EMPTY);
+            break;
+          }
+          const uint32_t bar = smem_u32(&ctl->full[s]);
+          if (elect_one()) {
+            load_w(dst, bar, mx_block(tile, kb, g.n_kb));
+            if (!kOwn) load_x(dst, bar, z * g.n_kb + kb);
+          }
+          __syncwarp();
+        }
+        dst += stage_bytes;
+        if (++s == g.stages) { s = 0; ph ^= 1; dst = smem_u32(smem); }
+      }
+      hi -= t.kb1 - t.kb0;
+    }
+    // whatever becomes of the other roles, this CTA's shared memory stays until its last copies have arrived
+    for (int i = max(0, it - g.stages); i < it; ++i)
+      if (!mbar_wait(smem_u32(&ctl->full[i % g.stages]), (i / g.stages) & 1)) break;
     __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------------ products
-    const uint32_t idesc = umma_idesc_bf16(kMxTileN, ncols);
+    const uint32_t idesc = umma_idesc_mx(kMxTileN, ncols);
     bool ok = true;
-    int s = 0, t = 0;
-    uint32_t ph = 0, tp = 0;
-    for (int it = 0; it < nkb; ++it) {
-      // (the widened weights come from this stage's codes, so the activations are here too, but this thread has to have seen it)
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->full[s]), ph) && mbar_wait(smem_u32(&ctl->wide_full[t]), tp))) {
-        if (lane == 0) mx_error(g, DEV_TIMEOUT_FULL);
+    int s = 0, j = 0;
+    uint32_t ph = 0;
+    for (long long hi = u1; ok && hi > u0; ++j) {
+      const ProdSeg t = prod_seg(g, u0, hi);
+      const int b = n_acc == 2 ? j & 1 : 0, use = n_acc == 2 ? j >> 1 : j;
+      const uint32_t d = tmem_base + b * acc_cols;
+      // the accumulator's previous tile has been read out
+      if (use > 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_empty[b]), (use - 1) & 1))) {
+        if (lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
         ok = false;
-        break;
       }
-      tc_fence_after();
-      const uint32_t sa = smem_u32(smem + (size_t)s * stage_bytes);
-      const uint64_t db0 = umma_desc_sw128(sa), db1 = umma_desc_sw128(sa + box_bytes);
-      if (elect_one()) {
-#pragma unroll
-        for (int i = 0; i < WT; ++i) {
-#pragma unroll
-          for (int kk = 0; kk < kMxTileK / 16; ++kk)
-            umma_f16_ts(tmem_base + i * acc_cols, wide_base + (t * WT + i) * kWideCols + kk * 8, (kk < 4 ? db0 : db1) + 2 * (kk & 3), idesc,
-                        (it | kk) != 0);
-        }
-        umma_commit(smem_u32(&ctl->empty[s]));
-        umma_commit(smem_u32(&ctl->wide_empty[t]));
-      }
-      __syncwarp();
-      if (++s == g.stages) { s = 0; ph ^= 1; }
-      if (++t == kMxWide) { t = 0; tp ^= 1; }
-    }
-    if (elect_one()) {
-      if (!ok) *reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) = 1;
-      umma_commit(smem_u32(&ctl->tmem_full));
-    }
-    __syncwarp();
-  } else {
-    // ------------------------------------------------------------------ widening, then the sums
-    const int sub = (warp - 2) >> 2;              // weight tile of the CTA
-    const int q = warp & 3;                       // TMEM lane quarter this warp may use
-    const int row = q * 32 + lane;
-    const uint32_t tq = (uint32_t)(q * 32) << 16;
-    bool ok = true;
-    {
-      int s = 0, t = 0;
-      uint32_t ph = 0, tp = 1;
-      for (int it = 0; it < nkb; ++it) {
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->full[s]), ph))) {
-          if (lane == 0) mx_error(g, DEV_TIMEOUT_FULL);
-          ok = false;
-          break;
-        }
-        const uint32_t wb = smem_u32(smem + (size_t)s * stage_bytes + act_bytes) + sub * kMxTileBytes;
-        uint4 codes[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) codes[j] = ld_shared_v4(wb + j * (kMxTileN * 16) + row * 16);
-        uint32_t sc;
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc) : "r"(wb + kMxCodeBytes + row * 4) : "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->empty[s]));
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->wide_empty[t]), tp))) {
-          if (lane == 0) mx_error(g, DEV_TIMEOUT_TMEM);
-          ok = false;
+      // Two blocks per round of the loop: of the 600 cycles that a block took by itself, longer than its share of the memory's time, 230 went
+      // into its six instructions, the others into waiting, electing and walking.
+      for (int kb = t.kb0; ok && kb < t.kb1;) {
+        const bool pair = g.stages >= 4 && kb + 1 < t.kb1, wrap = s + 1 == g.stages;   // (a short ring would wait for two copies)
+        const int s1 = wrap ? 0 : s + 1;
+        const uint32_t ph1 = wrap ? ph ^ 1 : ph;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->full[s]), ph) && (!pair || mbar_wait(smem_u32(&ctl->full[s1]), ph1)));
+        if (!ok) {
+          if (lane == 0) prod_error(g, DEV_TIMEOUT_FULL);
           break;
         }
         tc_fence_after();
-        const uint32_t dst = wide_base + (t * WT + sub) * kWideCols + tq;
-        // (scales above 2^1 need a second factor: rare, so the warp is asked once)
-        const bool large = __any_sync(0xffffffffu, (sc & 0x80808080u) != 0 && __vmaxu4(sc, 0x80808080u) != 0x80808080u);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t s8 = (sc >> (8 * j)) & 255u, mul = mx_factor(s8);
-          uint32_t r[16];
-          mx_unpack(codes[j].x, mul, r);
-          mx_unpack(codes[j].y, mul, r + 4);
-          mx_unpack(codes[j].z, mul, r + 8);
-          mx_unpack(codes[j].w, mul, r + 12);
-          if (large) {
-            const uint32_t more = mx_factor2(s8);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) r[i] = bf16x2_mul(r[i], more);
+        const uint32_t a0 = smem_u32(smem) + s * stage_bytes, a1 = smem_u32(smem) + s1 * stage_bytes;
+        if (elect_one()) {
+          prod_block(a0, scales + s * set_cols, d, idesc, act_bytes, sb_words, kb != t.kb0);
+          umma_commit(smem_u32(&ctl->empty[s]));
+          if (pair) {
+            prod_block(a1, scales + s1 * set_cols, d, idesc, act_bytes, sb_words, true);
+            umma_commit(smem_u32(&ctl->empty[s1]));
           }
-          tmem_st16(dst + j * 16, r);
         }
-        tmem_wait_st();
-        tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->wide_full[t]));
+        kb += 1 + pair;
+        if (pair) {
+          s = s1;
+          ph = ph1;
+        }
         if (++s == g.stages) { s = 0; ph ^= 1; }
-        if (++t == kMxWide) { t = 0; tp ^= 1; }
       }
+      if (elect_one()) {
+        if (!ok) *reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) = 1;
+        umma_commit(smem_u32(&ctl->acc_full[b]));
+      }
+      __syncwarp();
+      hi -= t.kb1 - t.kb0;
     }
-    pdl_wait();   // outputs of this kernel may still be read by the previous one's consumers
-    // The sums go through the ring's shared memory (free by now: every load was consumed by a product that has completed) to
-    // [tile][row m][128 features]; then a warp takes every fourth row with four consecutive features per lane.  With the K slices
-    // in one cluster the rows are dealt out over its CTAs, which add the slices' sums in slice order: the same order whatever the
-    // number of rows.
-    const bool done = mbar_wait(smem_u32(&ctl->tmem_full), 0);
-    if (!done && lane == 0) mx_error(g, DEV_TIMEOUT_TMEM);
-    ok = __all_sync(0xffffffffu, ok && done);
-    tc_fence_after();
-    ok = ok && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
-    const uint32_t taddr = tmem_base + sub * acc_cols + tq;
-    const uint32_t stg = smem_u32(smem) + sub * (g.Mc * kMxTileN * 4);
-    for (int c0 = 0; ok && c0 < M; c0 += 8) {
-      uint32_t r[8];
-      float v[8];
-      tmem_ld8(taddr + c0, r);
-      tmem_wait_ld();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r[j]);
-      for (int p = 1; p < g.planes; ++p) {
-        tmem_ld8(taddr + p * g.Mc + c0, r);
-        tmem_wait_ld();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(r[j]);
+  } else if (kStream) {
+    // ------------------------------------------------------------------ epilogue of a run
+    // Thread <-> feature out of tensor memory; through shared memory, eight rows at a time, to a warp per row with four features per
+    // lane, so that what goes out is whole lines.
+    const int q = warp & 3;                       // TMEM lane quarter this warp may read
+    const uint32_t stg = smem_u32(staging);
+    pdl_wait();   // (flags are cleared by the kernel before; outputs may still be read by its consumers)
+    int j = 0, turn = 0;
+    bool alive = true;   // (all warps go through the same barriers whatever becomes of a wait; after one has expired none is waited for)
+    for (long long hi = u1; hi > u0; ++j) {
+      const ProdSeg t = prod_seg(g, u0, hi);
+      const int b = n_acc == 2 ? j & 1 : 0, use = n_acc == 2 ? j >> 1 : j;
+      bool ok = alive && __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_full[b]), use & 1));
+      if (!ok && lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
+      alive = ok;
+      tc_fence_after();
+      ok = ok && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
+      const int tile = t.item / g.chunks, z = t.item - tile * g.chunks, m0 = z * g.Mc, M = min(g.Mc, g.M - m0);
+      const bool whole = t.kb1 == g.n_kb;         // this CTA finishes the tile
+      int before = cta;                           // CTAs [before, cta) have its earlier k-blocks
+      if (whole && t.kb0 > 0) {
+        const long long first = (long long)t.item * g.n_kb;
+        do --before;
+        while (prod_start(g, before, G) > first);
+        for (int c = before; ok && c < cta; ++c) ok = __all_sync(0xffffffffu, wait_flag(g.flags + c));
+        if (!ok && lane == 0) prod_error(g, DEV_TIMEOUT_GRID);
       }
+      const uint32_t taddr = tmem_base + b * acc_cols + ((uint32_t)(q * 32) << 16);
+      const int n = tile * kMxTileN + lane * 4;
+      for (int c0 = 0; c0 < M; c0 += 8, turn ^= 1) {
+        const uint32_t buf = stg + turn * (kProdStaging / 2);
+        float v[8];
+        prod_sums(g, taddr + c0, v);
+        if (c0 + 8 >= M) {   // (the sums are out of tensor memory)
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[b]));
+        }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) st_shared_f32(stg + ((c0 + j) * kMxTileN + row) * 4, v[j]);
+        for (int i = 0; i < 8; ++i) st_shared_f32(buf + (i * kMxTileN + q * 32 + lane) * 4, v[i]);
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        for (int i = warp - 2; i < 8 && c0 + i < M; i += 4) {
+          const uint4 u = ld_shared_v4(buf + (i * kMxTileN + lane * 4) * 4);
+          if (!ok) continue;
+          if (!whole) {
+            __stcg(reinterpret_cast<uint4 *>(g.slabs + ((size_t)cta * g.Mc + c0 + i) * kMxTileN) + lane, u);
+            continue;
+          }
+          float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+          if (before < cta) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int c = before; c < cta; ++c) {
+              const float4 p = __ldcg(reinterpret_cast<const float4 *>(g.slabs + ((size_t)c * g.Mc + c0 + i) * kMxTileN) + lane);
+              sum.x += p.x; sum.y += p.y; sum.z += p.z; sum.w += p.w;
+            }
+            w[0] += sum.x; w[1] += sum.y; w[2] += sum.z; w[3] += sum.w;
+          }
+          mx_finish<EPI>(g, m0 + c0 + i, n, w, lane);
+        }
+      }
+      if (!whole) {
+        __threadfence();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (warp == 2 && lane == 0 && ok) asm volatile("st.release.gpu.global.b32 [%0], %1;" ::"l"(g.flags + cta), "r"(1) : "memory");
+      }
+      hi -= t.kb1 - t.kb0;
+    }
+  } else if (warp < 6) {
+    // ------------------------------------------------------------------ epilogue of a tile
+    // The sums go through the ring's shared memory (free by now: every copy was consumed by a product that has completed) to
+    // [row][128 features]; then a warp takes every fourth row with four consecutive features per lane.  The rows are dealt out over the
+    // CTAs of a cluster, which add the slices' sums in slice order.
+    const int q = warp & 3, item = cta, tile = item / g.chunks, m0 = (item - tile * g.chunks) * g.Mc, M = min(g.Mc, g.M - m0);
+    pdl_wait();   // outputs of this kernel may still be read by the previous one's consumers
+    const bool done = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_full[0]), 0));
+    if (!done && lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
+    tc_fence_after();
+    const bool ok = done && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
+    const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16), stg = smem_u32(smem);
+    for (int c0 = 0; ok && c0 < M; c0 += 8) {
+      float v[8];
+      prod_sums(g, taddr + c0, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) st_shared_f32(stg + ((c0 + i) * kMxTileN + q * 32 + lane) * 4, v[i]);
     }
     if (C > 1) {
       __syncwarp();
       cluster_arrive();
       cluster_wait();
     } else {
-      asm volatile("bar.sync 1, %0;" ::"n"(128 * WT) : "memory");
+      asm volatile("bar.sync 1, 128;" ::: "memory");
     }
     const int rows_per = (M + C - 1) / C, m_beg = split * rows_per, m_end = min(M, m_beg + rows_per);
-    const int n = (tile0 + sub) * kMxTileN + lane * 4;
-    if (ok && sub < nt) {
-      for (int m = m_beg + (warp - 2 & 3); m < m_end; m += 4) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        const uint32_t at = stg + (m * kMxTileN + lane * 4) * 4;
-        if (C == 1) {
-          const uint4 u = ld_shared_v4(at);
-          v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
-        } else {
-          float4 p[8];
+    const int n = tile * kMxTileN + lane * 4;
+    for (int m = m_beg + warp - 2; ok && m < m_end; m += 4) {
+      const uint32_t at = stg + (m * kMxTileN + lane * 4) * 4;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (C == 1) {
+        const uint4 u = ld_shared_v4(at);
+        v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w);
+      } else {
+        float4 p[8];
 #pragma unroll
-          for (int c = 0; c < 8; ++c)
-            if (c < C) p[c] = ld_cluster_v4(at, c);
+        for (int c = 0; c < 8; ++c)
+          if (c < C) p[c] = ld_cluster_v4(at, c);
 #pragma unroll
-          for (int c = 0; c < 8; ++c)
-            if (c < C) { v[0] += p[c].x; v[1] += p[c].y; v[2] += p[c].z; v[3] += p[c].w; }
+        for (int c = 0; c < 8; ++c)
+          if (c < C) { v[0] += p[c].x; v[1] += p[c].y; v[2] += p[c].z; v[3] += p[c].w; }
+      }
+      mx_finish<EPI>(g, m0 + m, n, v, lane);
+    }
+  } else if (kOwn) {
+    // ------------------------------------------------------------------ planes
+    // A warp to a block, four blocks at a time (one block's chain of conversions takes about a thousand cycles): sixteen threads to a row,
+    // eight columns each.
+    typedef typename MxElem<TYPE>::raw raw;
+    constexpr int kWarps = 4, kAhead = 2;   // a warp's blocks whose columns are on their way
+    const int m = lane >> 4, col = (lane & 15) * 8, kb0 = (int)(u0 - first), nkb = (int)(u1 - u0);
+    const bool there = m < g.M;
+    const raw *row = (const raw *)g.x + (size_t)m * g.ldx;
+    pdl_wait();
+    MxRaw8<TYPE> x[kAhead];
+    int i = warp - 6;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) mx_fetch8<TYPE>(row, there && i + j * kWarps < nkb, (kb0 + i + j * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
+    for (bool ok = true; ok && i < nkb;) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (!ok || i >= nkb) break;
+        float v[8];
+        mx_widen8<TYPE>(x[j], v);
+        mx_fetch8<TYPE>(row, there && i + kAhead * kWarps < nkb, (kb0 + i + kAhead * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
+        const int s = i % g.stages;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->empty[s]), ((i / g.stages) & 1) ^ 1));
+        if (!ok) {
+          if (lane == 0) prod_error(g, DEV_TIMEOUT_EMPTY);
+          break;
         }
-        const long long mg = m0 + m;
-        if constexpr (EPI == MX_STORE) {
-          if (g.y_type == MX_F32) {
-            float *d = (float *)g.y + mg * g.ldy + n;
-            if (g.vec && n + 4 <= g.N) {
-              *reinterpret_cast<float4 *>(d) = make_float4(v[0], v[1], v[2], v[3]);
-            } else {
-              for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = v[j];
-            }
-          } else {
-            uint16_t h[4];
-            for (int j = 0; j < 4; ++j)
-              h[j] = g.y_type == MX_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v[j])) : __half_as_ushort(__float2half_rn(v[j]));
-            uint16_t *d = (uint16_t *)g.y + mg * g.ldy + n;
-            if (g.vec && n + 4 <= g.N) {
-              *reinterpret_cast<uint2 *>(d) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-            } else {
-              for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = h[j];
-            }
-          }
-        } else if constexpr (EPI == MX_LOGITS) {
-          *reinterpret_cast<float4 *>(g.out + (size_t)mg * g.N + n) = make_float4(v[0], v[1], v[2], v[3]);
-          // order-preserving map of the float to an unsigned word; ties resolve to the lowest id (lowest lane, then
-          // lowest of its four)
-          uint32_t best = 0;
-          int bi = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t u = __float_as_uint(v[j]);
-            u = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-            if (u > best) { best = u; bi = j; }
-          }
-          const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-          if (lane == __ffs(__ballot_sync(0xffffffffu, best == top)) - 1)
-            atomicMax(g.amax + (size_t)mg * kAmaxStride, ((unsigned long long)top << 32) | (unsigned long long)(0xFFFFFFFFu - (uint32_t)(n + bi)));
-        } else {  // MX_SWIGLU: even feature row = gate_f, odd = up_f, f = n / 2
-          __nv_bfloat16 h0, l0, h1, l1;
-          split_bf16(v[0] / (1.f + __expf(-v[0])) * v[1], h0, l0);
-          split_bf16(v[2] / (1.f + __expf(-v[2])) * v[3], h1, l1);
-          const int F = g.N >> 1, f = n >> 1;
-          *reinterpret_cast<__nv_bfloat162 *>(g.act_out + (size_t)mg * F + f) = __halves2bfloat162(h0, h1);
-          if (g.out_planes == 2)
-            *reinterpret_cast<__nv_bfloat162 *>(g.act_out + ((size_t)g.act_rows + mg) * F + f) = __halves2bfloat162(l0, l1);
-        }
+        mx_to_planes(v, there, smem + (size_t)s * stage_bytes + kProdW, act_bytes, g.Mc, g.planes, m, col);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->full[s]));
+        i += kWarps;
       }
     }
   }
-  if (C > 1) {
-    // (every thread of the cluster takes part in both barriers: the sums are in shared memory, then: nobody reads mine any more)
-    __syncwarp();
-    if (warp < 2) {
+  if constexpr (!kStream) {
+    if (C > 1) {
+      // (every thread of the cluster takes part in both barriers: the sums are in shared memory, then: nobody reads mine any more)
+      __syncwarp();
+      if (warp < 2 || warp >= 6) {
+        cluster_arrive();
+        cluster_wait();
+      }
       cluster_arrive();
       cluster_wait();
     }
-    cluster_arrive();
-    cluster_wait();
   }
   tc_fence_before();
   __syncthreads();
@@ -353,30 +466,49 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_a, const MxArgs g) {
   if (threadIdx.x == 0 && g.stamp) stamp_max(g.stamp + 3);
 }
 
-static size_t mx_stage_bytes(int wt, int planes, int Mc) {
-  return ((size_t)2 * planes * Mc * 128 + wt * kMxTileBytes + 1023) & ~(size_t)1023;
+// (elements of the weights, their scales, the activations' block as it lies in memory: both operands on 1024-byte boundaries)
+static size_t prod_stage_bytes(int planes, int Mc) {
+  const int ncols = planes * Mc;
+  return kProdW + ((512 + mx_x_block(ncols) + 1023) & ~1023);
 }
 
-template <int WT, int EPI>
-static cudaError_t mx_launch_one(const CUtensorMap &ta, const MxArgs &g, dim3 grid, size_t smem, cudaStream_t st, bool pdl) {
+// Rows per chunk: all of them up to 224 instruction columns, else equal chunks of fewer.  Then CTAs, two to an SM: runs of k-blocks where
+// there are more tiles than places, else clusters of as many as there is room for, eight at most.
+constexpr int kOwnRows = 2;   // most rows whose planes the product makes itself
+MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms) {
+  MxPlan p{};
+  const int step = planes % 2 ? 16 : 8, most = kProdAcc / planes / step * step;   // (the instruction's N, planes x rows, is a multiple of 16)
+  p.chunks = (M + most - 1) / most;
+  p.Mc = ((M + p.chunks - 1) / p.chunks + step - 1) / step * step;
+  p.chunks = (M + p.Mc - 1) / p.Mc;
+  const long long items = (long long)tiles * p.chunks, places = (long long)kProdCtas * n_sms;
+  p.stream = items > places && p.chunks == 1;
+  p.cluster = p.stream ? 1 : (int)std::max<long long>(1, std::min<long long>(std::min(8, n_kb), places / items));
+  p.ctas = (int)(p.stream ? places : items);
+  p.own = !p.stream && M <= kOwnRows;
+  return p;
+}
+
+template <int EPI, bool kStream, bool kOwn, int TYPE>
+static cudaError_t prod_launch_one(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
   static PerDeviceOnce once;
   int dev = -1;
   if (once.needed(&dev)) {
-    cudaError_t e = cudaFuncSetAttribute(mx_product_kernel<WT, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    cudaError_t e = cudaFuncSetAttribute(mx_product_kernel<EPI, kStream, kOwn, TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     if (e != cudaSuccess) return e;
     once.done(dev);
   }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(64 + 128 * WT);
+  cfg.gridDim = dim3(p.ctas, p.cluster);
+  cfg.blockDim = dim3(kOwn ? 320 : 192);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   int n = 0;
-  if (grid.y > 1) {
+  if (p.cluster > 1) {
     at[n].id = cudaLaunchAttributeClusterDimension;
     at[n].val.clusterDim.x = 1;
-    at[n].val.clusterDim.y = grid.y;
+    at[n].val.clusterDim.y = p.cluster;
     at[n].val.clusterDim.z = 1;
     ++n;
   }
@@ -387,41 +519,36 @@ static cudaError_t mx_launch_one(const CUtensorMap &ta, const MxArgs &g, dim3 gr
   }
   cfg.attrs = at;
   cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, mx_product_kernel<WT, EPI>, ta, g);
+  return cudaLaunchKernelEx(&cfg, mx_product_kernel<EPI, kStream, kOwn, TYPE>, tw, g);
 }
 
-MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms) {
-  MxPlan p;
-  const int step = planes == 1 ? 16 : 8, most = 128 / planes;   // (the instruction's N, planes x rows, is a multiple of 16)
-  p.Mc = std::min(most, (M + step - 1) / step * step);
-  p.tiles_per_cta = p.Mc * planes > 32 ? 2 : 1;
-  const int groups = (tiles + p.tiles_per_cta - 1) / p.tiles_per_cta * ((M + p.Mc - 1) / p.Mc), room = p.tiles_per_cta == 1 ? 2 * n_sms : n_sms;
-  p.cluster = std::max(1, std::min(std::min(8, n_kb), room / std::max(1, groups)));
-  return p;
+template <int EPI>
+static cudaError_t prod_launch(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
+  if (p.stream) return prod_launch_one<EPI, true, false, 0>(tw, g, p, smem, st, pdl);
+  if (!p.own) return prod_launch_one<EPI, false, false, 0>(tw, g, p, smem, st, pdl);
+  switch (g.x_type) {
+    case MX_BF16: return prod_launch_one<EPI, false, true, MX_BF16>(tw, g, p, smem, st, pdl);
+    case MX_F16: return prod_launch_one<EPI, false, true, MX_F16>(tw, g, p, smem, st, pdl);
+    default: return prod_launch_one<EPI, false, true, MX_F32>(tw, g, p, smem, st, pdl);
+  }
 }
 
-cudaError_t launch_mx_product(int epi, const CUtensorMap &ta, MxArgs g, int wt, int cluster, cudaStream_t st, bool pdl) {
-  const size_t stage = mx_stage_bytes(wt, g.planes, g.Mc);
-  const size_t limit = (wt == 1 ? 113 : 227) * 1024 - sizeof(MxSmemCtl);
-  g.stages = (int)std::min<size_t>(kMxMaxStages, limit / stage);
-  const size_t smem = g.stages * stage + sizeof(MxSmemCtl);
-  // the sums pass through the ring; both weight tiles' sums and widened blocks share the 512 columns of tensor memory
-  if (wt < 1 || wt > 2 || g.stages < 2 || g.Mc % 8 || (g.planes * g.Mc) % 16 || g.planes * g.Mc > 256 || cluster < 1 || cluster > 8 ||
-      cluster > g.n_kb || wt * (((g.planes * g.Mc + 31) & ~31) + kMxWide * kWideCols) > 512 || (size_t)g.stages * stage < (size_t)wt * g.Mc * kMxTileN * 4)
+cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxPlan &p, cudaStream_t st, bool pdl) {
+  g.Mc = p.Mc; g.chunks = p.chunks;
+  g.units = (long long)g.tiles * g.chunks * g.n_kb;
+  const size_t stage = prod_stage_bytes(g.planes, g.Mc), fixed = kProdStaging + sizeof(ProdSmemCtl);
+  g.stages = (int)std::min<size_t>(kProdMaxStages, (113 * 1024 - fixed) / stage);
+  const int ncols = g.planes * g.Mc;
+  const int acc = (ncols + 31) & ~31, sets = g.stages * (4 + 4 * ((ncols + 127) / 128));   // columns of an accumulator, of all scales
+  g.n_acc = p.stream && 2 * acc + sets <= 256 ? 2 : 1;
+  if (g.stages < 2 || g.Mc % 8 || ncols % 16 || ncols > kProdAcc || g.n_acc * acc + sets > 256 || p.ctas < 1 || p.cluster < 1 || p.cluster > 8 || p.cluster > g.n_kb ||
+      (p.stream && p.ctas > g.units) || (size_t)g.stages * stage < (size_t)g.Mc * kMxTileN * 4)
     return cudaErrorInvalidValue;
-  const dim3 grid((g.tiles + wt - 1) / wt, cluster, (g.M + g.Mc - 1) / g.Mc);
-  if (wt == 1) {
-    switch (epi) {
-      case MX_STORE: return mx_launch_one<1, MX_STORE>(ta, g, grid, smem, st, pdl);
-      case MX_SWIGLU: return mx_launch_one<1, MX_SWIGLU>(ta, g, grid, smem, st, pdl);
-      case MX_LOGITS: return mx_launch_one<1, MX_LOGITS>(ta, g, grid, smem, st, pdl);
-    }
-  } else {
-    switch (epi) {
-      case MX_STORE: return mx_launch_one<2, MX_STORE>(ta, g, grid, smem, st, pdl);
-      case MX_SWIGLU: return mx_launch_one<2, MX_SWIGLU>(ta, g, grid, smem, st, pdl);
-      case MX_LOGITS: return mx_launch_one<2, MX_LOGITS>(ta, g, grid, smem, st, pdl);
-    }
+  const size_t smem = g.stages * stage + fixed;
+  switch (epi) {
+    case MX_STORE: return prod_launch<MX_STORE>(tw, g, p, smem, st, pdl);
+    case MX_SWIGLU: return prod_launch<MX_SWIGLU>(tw, g, p, smem, st, pdl);
+    case MX_LOGITS: return prod_launch<MX_LOGITS>(tw, g, p, smem, st, pdl);
   }
   return cudaErrorInvalidValue;
 }

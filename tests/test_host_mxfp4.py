@@ -44,15 +44,18 @@ def test_conversions_refuse():
 
 def test_product_refuses():
     L = B.lib()
-    good = dict(rows=4, n=100, k=64, ldx=64, ldy=100, x_type=0, y_type=2, matrix=P, x=P, y=P)
+    good = dict(rows=4, ldx=64, ldy=100, x_type=0, y_type=2, x=P, y=P)
 
-    def call(**over):
+    def call(n=100, k=64, **over):
+        m = B.ts_mxfp4_matrix(n, k, P)
         a = B.ts_mxfp4_product_args()
+        a.matrix = C.pointer(m)
         for name, v in {**good, **over}.items():
             setattr(a, name, v)
         return L.ts_mxfp4_product(C.byref(a), None)
 
     _refused(L.ts_mxfp4_product(None, None), "null")
+    _refused(L.ts_mxfp4_product(C.byref(B.ts_mxfp4_product_args()), None), "null")
     _refused(call(x_type=5), "element type")
     _refused(call(y_type=-1), "element type")
     _refused(call(rows=-4), "sides")
@@ -64,16 +67,29 @@ def test_product_refuses():
     _refused(call(y=P + 2), "aligned")
     _refused(call(status=P + 2), "status")
     assert call(rows=0) == 0 and call(n=0, ldy=0) == 0      # nothing to do
+    _refused(L.ts_mxfp4_matrix_init(None, P, 4, 64), "null")
+    m = B.ts_mxfp4_matrix()
+    _refused(L.ts_mxfp4_matrix_init(C.byref(m), P + 64, 4, 64), "aligned")
+    _refused(L.ts_mxfp4_matrix_init(C.byref(m), P, -1, 64), "sides")
+    assert L.ts_mxfp4_matrix_init(C.byref(m), None, 0, 64) == 0 and (m.n, m.k) == (0, 64)
 
 
 def test_sizes():
-    L, n = B.lib(), C.c_uint64()
-    size = lambda f, *a: (f(*a, C.byref(n)), n.value)
+    L = B.lib()
+    out = C.c_uint64()
+    size = lambda f, *a: (f(*a, C.byref(out)), out.value)
     assert size(L.ts_mxfp4_matrix_bytes, 128, 128) == (0, 8704)
     assert size(L.ts_mxfp4_matrix_bytes, 129, 1) == (0, 2 * 8704)
     assert size(L.ts_mxfp4_matrix_bytes, 0, 5) == (0, 0)
-    assert size(L.ts_mxfp4_product_workspace, 3, 100, 33, 2)[1] >= 2 * 3 * 40 * 2
-    assert L.ts_mxfp4_product_workspace(3, 100, 33, 7, C.byref(n)) == -1
+    # room for fewer rows too: what is asked for the most is never less than what is asked for fewer
+    for x_type in (0, 1, 2):
+        for n in (100, 5000, 151936):
+            most = 0
+            for rows in list(range(0, 300)) + [1024, 5000]:
+                code, b = size(L.ts_mxfp4_product_workspace, rows, n, 4100, x_type)
+                assert code == 0 and b >= most
+                most = b
+    assert L.ts_mxfp4_product_workspace(3, 100, 33, 7, C.byref(out)) == -1
 
 
 def test_reference_rounds_by_hand():
