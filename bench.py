@@ -257,7 +257,7 @@ def max_over_ranks(value_ms: float, world: int, backend_device=None) -> float:
     return float(t[0])
 
 
-def build_gpu_model(shape, lens, ks, act_split=True, path=0, extra_ctx=0):
+def build_gpu_model(shape, lens, ks, act_split=True, path=0, extra_ctx=0, weights="bf16"):
     """Random-init weights generated on the device (N(0, 0.02) rounded to bf16, gains one) and a KV
     pool filled with N(0,1) fp16 values; sessions placed at their context lengths.  The model's capacity is the
     workload's: context + 2 k_max positions per sequence (+ extra_ctx for the decode-loop trace, which generates
@@ -269,7 +269,7 @@ def build_gpu_model(shape, lens, ks, act_split=True, path=0, extra_ctx=0):
     max_ctx = max(lens) + 2 * k_max + extra_ctx
     pages = sum((n + 2 * k_max + extra_ctx + 15) // 16 for n in lens) + 8
     m = ts.Model(shape, max_pages=pages, max_batch=B_, k_max=k_max, max_rows=max(sum(ks), k_max),
-                 max_ctx=max_ctx, act_split=act_split, path=path)
+                 max_ctx=max_ctx, act_split=act_split, path=path, weights=weights)
     g = torch.Generator(device="cuda").manual_seed(260413519)
     s = shape
 
@@ -465,6 +465,7 @@ def main():
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-act-split", action="store_true")
     ap.add_argument("--path", type=int, default=0, help="0 auto, 1 one kernel per stage, 2 single persistent kernel")
+    ap.add_argument("--weights", default="bf16", choices=["bf16", "mxfp4"], help="how the projection matrices are held")
     ap.add_argument("--retrieval", type=int, default=0,
                     help="N > 0: time ts_topk_cosine (K = 10) over N synthetic hidden states of the workload's width "
                          "instead of the verify step, and print its own JSON line")
@@ -508,7 +509,7 @@ def main():
         dist.init_process_group("nccl", device_id=torch.device("cuda", local_rank))
     ts.binding.lib()
     planes = 1 if args.no_act_split else 2
-    model, sessions = build_gpu_model(shape, lens, ks, act_split=not args.no_act_split, path=args.path)
+    model, sessions = build_gpu_model(shape, lens, ks, act_split=not args.no_act_split, path=args.path, weights=args.weights)
     M = sum(ks)
     drafts = [[64 + (7 * j + i) % (shape.vocab - 64) for j in range(k - 1)] for i, k in enumerate(ks)]
     stream = torch.cuda.current_stream()
@@ -632,7 +633,7 @@ def main():
         # the trace generates TRACE_TOKENS tokens: it gets a model of its own with room for them (the timed model
         # above has the capacity of the workload it is timed on)
         model.close()
-        model, sessions = build_gpu_model(shape, lens, ks, act_split=not args.no_act_split, path=args.path,
+        model, sessions = build_gpu_model(shape, lens, ks, act_split=not args.no_act_split, path=args.path, weights=args.weights,
                                           extra_ctx=TRACE_TOKENS)
         sessions[0].close()                      # its pages go back to the pool; the trace takes a session of its own
         trace = run_loop_trace(model, lens[0], 3, model.cfg.k_max, args.trace_jsonl)

@@ -71,7 +71,12 @@ typedef struct {
   int32_t act_split;   /* 1: GEMM activations are fed as a bf16 (hi, lo) pair; 0: hi only */
   int32_t path;        /* 0: the library chooses; 1: one kernel per stage; 2: the single persistent kernel
                           (steps of at most 64 rows; a larger step fails with TS_ERR_K_TOO_LARGE) */
+  int32_t weights;     /* TS_WEIGHTS_BF16 or TS_WEIGHTS_MXFP4: how the projection matrices (Q, K, V, O, gate, up, down, LM head) are
+                          held.  MXFP4 (see below) takes 17 bytes for 32 weights instead of 64; the embedding table and the gains stay
+                          as they are; path must not be 2.  A row's results keep to the same rule as with bf16 weights: the same bits
+                          whatever the number of rows up to 64. */
 } ts_model_config;
+enum { TS_WEIGHTS_BF16 = 0, TS_WEIGHTS_MXFP4 = 1 };
 
 typedef struct {
   uint64_t weights_bytes;    /* device */
@@ -109,6 +114,11 @@ enum { TS_W_EMBED = 0, TS_W_LM_HEAD = 1, TS_W_FINAL_GAIN = 2, TS_W_Q = 3, TS_W_K
  * Errors: TS_ERR_ARG on a shape that does not match the configuration. */
 ts_status ts_load_tensor(ts_model *m, int32_t kind, int32_t layer, const void *host_data,
                          int64_t rows, int64_t cols);
+/* The same for a model whose weights are in MXFP4 and a projection matrix that is quantised already: codes and scales as
+ * ts_mxfp4_quantise leaves them (host or device).  Such a model's ts_load_tensor quantises the bf16 matrices that it is given
+ * (ts_mxfp4_quantise's rounding).  Errors: TS_ERR_STATE for a model with bf16 weights, TS_ERR_ARG for the embedding table and gains. */
+ts_status ts_load_tensor_mxfp4(ts_model *m, int32_t kind, int32_t layer, const void *codes, const void *scales, int64_t rows,
+                               int64_t cols);
 
 ts_status ts_model_destroy(ts_model *m);
 
@@ -294,7 +304,8 @@ ts_status ts_verify_tree_sampled(ts_model *m, ts_session *const *sessions, int32
 ts_status ts_verify_replay(ts_model *m);
 
 /* Run the last step once more and return, per class, the summed milliseconds and a count:
- * 0 projection GEMM (up to 80 rows, 96 with one plane, with norm, residual, rotary and KV append in it), 1 attention,
+ * 0 projection GEMM (up to 80 rows, 96 with one plane, with norm, residual, rotary and KV append in it; MXFP4 weights: and the
+ * kernels that prepare its input), 1 attention,
  * 2 attention merge, 3 norm / residual, 4 rotary + KV append, 5 acceptance, 6 the persistent kernel as a whole.  n_classes >= 6 (class 6 is written if
  * n_classes > 6).  With separate kernels an event follows every launch (no overlap between
  * kernels) and the count is the launches; with the persistent kernel classes 0..2 are sums of
@@ -506,7 +517,7 @@ ts_status ts_mxfp4_matrix_init(ts_mxfp4_matrix *m, const void *data, int64_t n, 
  * The tensor cores multiply the four-bit elements as they are; x goes in as a sum of 2 (bf16), 3 (fp16) or 5 (fp32) numbers of four
  * significant bits with a scale per 32 columns, which leaves out less than 2^-20 of the largest of the 32 (of bf16 and fp16 rows
  * nothing of elements down to 2^-13 of it); sums are fp32.  A row that holds an infinity or a NaN gives NaN.
- * A row's result depends on that row and on the matrix, not on the other rows: with up to 64 rows (fp32: 32) it is the same, bit for
+ * A row's result depends on that row and on the matrix, not on the other rows: with up to 64 rows it is the same, bit for
  * bit, whatever their number.  What lies between the rows of y is left as it is; y must not overlap x or the matrix.
  * workspace: device, 128-byte aligned, of ts_mxfp4_product_workspace bytes (host only call; enough for fewer rows too).  It holds nothing
  * between calls; calls that overlap on the GPU need one each.

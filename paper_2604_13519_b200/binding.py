@@ -17,6 +17,7 @@ TS_PAGE_SIZE = 16
 TS_FLAG_SKIP_LM_HEAD = 1
 TS_FLAG_WANT_TOPK = 2
 TS_TOPK = 8
+TS_WEIGHTS_BF16, TS_WEIGHTS_MXFP4 = 0, 1
 
 STATUS = {0: "TS_OK", -1: "TS_ERR_ARG", -2: "TS_ERR_STATE", -3: "TS_ERR_OOM_PAGES",
           -4: "TS_ERR_K_TOO_LARGE", -5: "TS_ERR_TOKEN_RANGE", -6: "TS_ERR_DEVICE_TIMEOUT",
@@ -37,7 +38,7 @@ class ts_model_config(C.Structure):
                                          "d_ffn", "vocab")] + \
                [("rope_theta", C.c_float), ("rms_eps", C.c_float)] + \
                [(n, C.c_int32) for n in ("max_pages", "max_batch", "k_max", "max_rows", "max_ctx",
-                                         "act_split", "path")]
+                                         "act_split", "path", "weights")]
 
 
 class ts_buffer_sizes(C.Structure):
@@ -104,6 +105,7 @@ _SIGNATURES = {
     "ts_query_buffer_sizes": [C.POINTER(ts_model_config), C.POINTER(ts_buffer_sizes)],
     "ts_init_model": [C.POINTER(ts_model_config), C.POINTER(ts_buffers), _P, C.POINTER(_P)],
     "ts_load_tensor": [_P, C.c_int32, C.c_int32, _P, C.c_int64, C.c_int64],
+    "ts_load_tensor_mxfp4": [_P, C.c_int32, C.c_int32, _P, _P, C.c_int64, C.c_int64],
     "ts_model_destroy": [_P],
     "ts_schema_create": [C.POINTER(ts_vocab_layout), C.POINTER(_P)],
     "ts_schema_add_tool": [_P, _I32P, C.c_int32, _I32P, _I32P, C.c_int32],
@@ -260,7 +262,7 @@ class Model:
     """ts_init_model + ts_load_tensor over buffers allocated with torch."""
 
     def __init__(self, shape, max_pages: int, max_batch: int, k_max: int, max_rows: int, max_ctx: int,
-                 act_split: bool = True, device="cuda:0", stream=None, path: int = 0):
+                 act_split: bool = True, device="cuda:0", stream=None, path: int = 0, weights: str = "bf16"):
         import torch
         self.torch = torch
         self.shape = shape
@@ -271,6 +273,7 @@ class Model:
         c.max_pages, c.max_batch, c.k_max, c.max_rows, c.max_ctx = max_pages, max_batch, k_max, max_rows, max_ctx
         c.act_split = 1 if act_split else 0
         c.path = path
+        c.weights = {"bf16": TS_WEIGHTS_BF16, "mxfp4": TS_WEIGHTS_MXFP4}[weights]
         self.cfg = c
         sizes = ts_buffer_sizes()
         _check(lib().ts_query_buffer_sizes(C.byref(c), C.byref(sizes)))
@@ -300,6 +303,14 @@ class Model:
         t = t.contiguous()
         rows, cols = (t.shape if t.dim() == 2 else (1, t.shape[0]))
         _check(lib().ts_load_tensor(self.h, kind, layer, _P(t.data_ptr()), rows, cols))
+
+    def load_tensor_mxfp4(self, kind: int, layer: int, codes, scales, cols: int):
+        """codes, scales: uint8 tensors as ts_mxfp4_quantise returns them, of a matrix of `cols` columns (host or device)."""
+        nb, rows = (cols + 31) // 32, codes.shape[0]
+        if tuple(codes.shape) != (rows, 16 * nb) or tuple(scales.shape) != (rows, nb):
+            raise ValueError(f"{cols} columns take codes of [rows][{16 * nb}] and scales of [rows][{nb}]")
+        codes, scales = codes.contiguous(), scales.contiguous()
+        _check(lib().ts_load_tensor_mxfp4(self.h, kind, layer, _P(codes.data_ptr()), _P(scales.data_ptr()), rows, cols))
 
     def load_weights(self, w: dict):
         """w: name -> CPU tensor, names as produced by the synthetic generator."""
@@ -343,7 +354,7 @@ class Model:
     def timeline(self):
         """[(class name, start, first wait return, last wait return, end)] per launch of the last step re-run under
         its normal launch configuration; times in microseconds from the first kernel's start."""
-        cap = 9 * self.shape.n_layers + 16
+        cap = 18 * self.shape.n_layers + 16
         st = (C.c_uint64 * (4 * cap))()
         cls = (C.c_int32 * cap)()
         n = C.c_int32(0)

@@ -13,6 +13,7 @@
 
 #include "drafter.h"
 #include "kernels.h"
+#include "mxfp4.h"
 #include "schedule.h"
 #include "toolspec.h"
 
@@ -85,7 +86,7 @@ struct Layout {
   int n_maps, n_counters, n_phases;
   StepIo step_io, prompt_io;   // of a verification step, of a piece of a prompt
   int in_ints, o_path, o_topk;
-  uint64_t samp_stats, topk_cand;
+  uint64_t samp_stats, topk_cand, mx;
   // step out (int32 offsets)
   int o_argmax, o_accept, o_emitted, o_newlen, o_newpend, o_err, o_done, out_ints;
   int rows_alloc;        // rows of the activation buffers: max_rows or a piece of a prompt, whichever is more
@@ -109,8 +110,16 @@ bool config_ok(const ts_model_config &c, const char **why) {
   REQ(c.act_split == 0 || c.act_split == 1, "act_split must be 0 or 1");
   REQ(c.path >= 0 && c.path <= 2, "path must be 0 (auto), 1 (separate kernels) or 2 (fused kernel)");
   REQ(c.rope_theta > 1.f && c.rms_eps > 0.f, "rope_theta / rms_eps out of range");
+  REQ(c.weights == TS_WEIGHTS_BF16 || c.weights == TS_WEIGHTS_MXFP4, "weights must be TS_WEIGHTS_BF16 or TS_WEIGHTS_MXFP4");
+  REQ(c.weights == TS_WEIGHTS_BF16 || c.path != 2, "the persistent kernel (path 2) takes bf16 weights only");
 #undef REQ
   return true;
+}
+
+// bytes of a stored projection matrix (mxfp4.h, or bf16 blocks of 128 x 64)
+uint64_t matrix_bytes(const ts_model_config &c, uint64_t N, uint64_t K) {
+  if (c.weights == TS_WEIGHTS_MXFP4) return N / ts::kMxTileN * ((K + ts::kMxTileK - 1) / ts::kMxTileK) * ts::kMxTileBytes;
+  return N * K * 2;
 }
 
 void make_layout(const ts_model_config &c, Layout *L) {
@@ -120,14 +129,14 @@ void make_layout(const ts_model_config &c, Layout *L) {
   uint64_t o = 0;
   auto take = [&](uint64_t bytes) { uint64_t r = o; o = align_up(o + bytes, 1024); return r; };
   L->embed = take(V * d * 2);
-  L->lm_head = take(V * d * 2);
+  L->lm_head = take(matrix_bytes(c, V, d));
   L->wqkv.resize(c.n_layers); L->wo.resize(c.n_layers); L->wgu.resize(c.n_layers); L->wd.resize(c.n_layers);
   L->g1.resize(c.n_layers); L->g2.resize(c.n_layers);
   for (int l = 0; l < c.n_layers; ++l) {
-    L->wqkv[l] = take((uint64_t)L->Nqkv * d * 2);
-    L->wo[l] = take(d * Nq * 2);
-    L->wgu[l] = take(2 * F * d * 2);
-    L->wd[l] = take(d * F * 2);
+    L->wqkv[l] = take(matrix_bytes(c, L->Nqkv, d));
+    L->wo[l] = take(matrix_bytes(c, d, Nq));
+    L->wgu[l] = take(matrix_bytes(c, 2 * F, d));
+    L->wd[l] = take(matrix_bytes(c, d, F));
   }
   for (int l = 0; l < c.n_layers; ++l) { L->g1[l] = take(d * 4); L->g2[l] = take(d * 4); }
   L->gf = take(d * 4);
@@ -208,8 +217,11 @@ void make_layout(const ts_model_config &c, Layout *L) {
   L->sync = take((uint64_t)(8 + L->n_counters) * 4);
   L->n_phases = 6 * c.n_layers + 3;
   L->phase_t = take((uint64_t)3 * L->n_phases * 8);
-  L->max_stamps = 9 * c.n_layers + 16;
+  L->max_stamps = 18 * c.n_layers + 16;   // (launches of a step: 9 per layer, in MXFP4 13, or 17 where rows go in two passes)
   L->stamps = take((uint64_t)L->max_stamps * 4 * 8);
+  L->mx = 0;
+  if (c.weights == TS_WEIGHTS_MXFP4)   // planes of the activations, sums of tiles that two CTAs share
+    L->mx = take(ts::mx_scratch_most((int)R, (int)((std::max(std::max(d, F), Nq) + ts::kMxTileK - 1) / ts::kMxTileK), ts::mx_planes_of(c.act_split ? ts::MX_PAIR : ts::MX_BF16)));
   L->workspace_bytes = o;
   L->host_io_bytes = align_up((uint64_t)(L->in_ints + L->out_ints + 2 * ts::kTopMax + 2) * 4, 4096);   // (and a retrieval's result pairs, status and number)
 }
@@ -336,7 +348,11 @@ ts_status make_map(EncodeTiledFn enc, CUtensorMap *out, void *base, int rank, co
 // Weights are stored block by block: the 128 x 64 block (tile t, k-block kb) of an [N][K] matrix is the
 // contiguous 16 KB at rows (t * K/64 + kb) * 128 .. of a [.][64] array.  One block is one TMA box and one run
 // of DRAM pages.
-ts_status weight_map(EncodeTiledFn enc, CUtensorMap *out, void *base, uint64_t N, uint64_t K) {
+ts_status weight_map(EncodeTiledFn enc, const ts_model_config &c, CUtensorMap *out, void *base, uint64_t N, uint64_t K) {
+  if (c.weights == TS_WEIGHTS_MXFP4) {
+    const int r = ts::mx_weight_map((void *)enc, out, base, N / ts::kMxTileN * ((K + ts::kMxTileK - 1) / ts::kMxTileK));
+    return r ? fail(TS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", r) : TS_OK;
+  }
   const uint64_t dims[2] = {64, N * (K / 64)};
   const uint32_t box[2] = {64, 128};
   return make_map(enc, out, base, 2, dims, box);
@@ -419,6 +435,29 @@ ts_status run_gemm_ws(ts_model *m, int epi, const CUtensorMap &tw, const CUtenso
   const int cluster = (epi == ts::EPI_QKV || epi == ts::EPI_RESID) ? pick_cluster(m, N / 128, g.n_kblocks) : 1;
   CU_TRY(ts::launch_gemm(epi, tw, ta[mi], g, cluster, m->gemm_smem_budget, m->st, m->use_pdl && !m->profiling));
   m->launched(0);
+  return TS_OK;
+}
+
+// A projection with an MXFP4 matrix: its input as planes of e4m3 numbers, then the product (mxfp4_product.cu).  x: bf16 planes [planes][R][K].
+ts_status run_mx(ts_model *m, int epi, const CUtensorMap &tw, uint64_t w, int N, int K, int M, const __nv_bfloat16 *x, float *out,
+                 __nv_bfloat16 *act_out, unsigned long long *amax) {
+  const Layout &L = m->L;
+  ts::MxArgs g{};
+  g.w = m->W(w); g.N = N; g.tiles = N / ts::kMxTileN; g.n_kb = (K + ts::kMxTileK - 1) / ts::kMxTileK;
+  g.err = m->d_out() + L.o_err;
+  g.y = out; g.ldy = N; g.y_type = ts::MX_F32; g.vec = 1;
+  g.out = out; g.act_out = act_out; g.act_rows = L.rows_alloc; g.out_planes = m->planes; g.amax = amax;
+  const ts::MxInput in{x, m->planes == 2 ? ts::MX_PAIR : ts::MX_BF16, M, K, K, (long long)L.rows_alloc * K};
+  const ts::MxPlan p = ts::mx_plan(M, g.tiles, g.n_kb, ts::mx_planes_of(in.type), m->n_sms);
+  const bool pdl = m->use_pdl && !m->profiling;
+  if (!p.own) {
+    CU_TRY(ts::launch_mx_input(in, m->WS(L.mx), p, m->st, pdl));
+    m->launched(0);
+  }
+  g.stamp = m->stamp_slot();
+  int n = 0;
+  CU_TRY(ts::launch_mx_product(epi, tw, g, in, m->WS(L.mx), p, m->st, pdl, &n));
+  for (int i = 0; i < n; ++i) m->launched(0);
   return TS_OK;
 }
 
@@ -541,8 +580,8 @@ ts_status run_step(ts_model *m) {
   m->launched(3);
   // Up to kFewRows rows the weight-streaming kernel: QKV rotates and appends K/V itself, O and down update the residual stream
   // and prepare the next projection's input (6 launches per layer); beyond, the many-rows kernel with its split-K slabs
-  // folded by a rotary and two norm kernels.
-  const bool few = M <= kFewRows[m->planes - 1];
+  // folded by a rotary and two norm kernels.  MXFP4 weights: the latter with one slab of finished sums.
+  const bool mx = c.weights == TS_WEIGHTS_MXFP4, few = !mx && M <= kFewRows[m->planes - 1];
   float *ss = (float *)m->WS(L.ss_part);
   const bool skip_head = (m->last_flags & TS_FLAG_SKIP_LM_HEAD) != 0;
   int splits = 0;
@@ -563,7 +602,9 @@ ts_status run_step(ts_model *m) {
                                    m->planes, m->st, m->stamp_slot()));
         m->launched(3);
       }
-      s = run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_qkv[l], m->tm_h, L.Nqkv, d, M, part, nullptr, nullptr, &splits);
+      splits = 1;
+      s = mx ? run_mx(m, ts::MX_STORE, m->tm_qkv[l], L.wqkv[l], L.Nqkv, d, M, h, part, nullptr, nullptr)
+             : run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_qkv[l], m->tm_h, L.Nqkv, d, M, part, nullptr, nullptr, &splits);
       if (s) return s;
       CU_TRY(ts::launch_rope_kv(in, part, splits, part_R, c.n_q_heads, c.n_kv_heads, c.head_dim, rope, q,
                                 q + (size_t)R * Nq, m->k_pages(l), m->v_pages(l), m->st, m->stamp_slot()));
@@ -602,15 +643,18 @@ ts_status run_step(ts_model *m) {
       s = run_gemm_ws(m, ts::EPI_RESID, m->tm_d[l], m->tm_act, d, F, M, g);
       if (s) return s;
     } else {
-      s = run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_o[l], m->tm_attn, d, Nq, M, part, nullptr, nullptr, &splits);
+      s = mx ? run_mx(m, ts::MX_STORE, m->tm_o[l], L.wo[l], d, Nq, M, attn, part, nullptr, nullptr)
+             : run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_o[l], m->tm_attn, d, Nq, M, part, nullptr, nullptr, &splits);
       if (s) return s;
       CU_TRY(ts::launch_add_norm(M, d, part, splits, part_R, (const float *)m->W(L.g2[l]), c.rms_eps, x, h, R,
                                  m->planes, m->st, m->stamp_slot()));
       m->launched(3);
       // (gate-up keeps its SwiGLU epilogue and so cannot split K)
-      s = run_gemm_rows(m, ts::EPI_SWIGLU, m->tm_gu[l], m->tm_h, 2 * F, d, M, nullptr, act, nullptr, nullptr);
+      s = mx ? run_mx(m, ts::MX_SWIGLU, m->tm_gu[l], L.wgu[l], 2 * F, d, M, h, nullptr, act, nullptr)
+             : run_gemm_rows(m, ts::EPI_SWIGLU, m->tm_gu[l], m->tm_h, 2 * F, d, M, nullptr, act, nullptr, nullptr);
       if (s) return s;
-      s = run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_d[l], m->tm_act, d, F, M, part, nullptr, nullptr, &splits);
+      s = mx ? run_mx(m, ts::MX_STORE, m->tm_d[l], L.wd[l], d, F, M, act, part, nullptr, nullptr)
+             : run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_d[l], m->tm_act, d, F, M, part, nullptr, nullptr, &splits);
       if (s) return s;
     }
   }
@@ -624,6 +668,8 @@ ts_status run_step(ts_model *m) {
     ts::GemmArgs g{};
     g.out = (float *)m->WS(L.logits); g.amax = amax;
     s = run_gemm_ws(m, ts::EPI_LOGITS, m->tm_lm, m->tm_h, c.vocab, d, M, g);
+  } else if (mx) {
+    s = run_mx(m, ts::MX_LOGITS, m->tm_lm, L.lm_head, c.vocab, d, M, h, (float *)m->WS(L.logits), nullptr, amax);
   } else {
     s = run_gemm_rows(m, ts::EPI_LOGITS, m->tm_lm, m->tm_h, c.vocab, d, M, (float *)m->WS(L.logits), nullptr, amax, nullptr);
   }
@@ -984,7 +1030,7 @@ ts_status stage_and_run(ts_model *m, ts_session *const *ss, int B, const std::ve
   }
   // All refusals come before the first word of the staged step's own state (last_*) changes: a replay after a refused call
   // runs the step that was staged last.
-  const bool can_fuse = m->fused_ok && M <= kFusedMaxRows;
+  const bool can_fuse = m->fused_ok && M <= kFusedMaxRows && c.weights == TS_WEIGHTS_BF16;
   if (c.path == 2 && !can_fuse)
     return fail(TS_ERR_K_TOO_LARGE, "the fused kernel takes at most %d rows on a device that supports it (step has %d)",
                 kFusedMaxRows, M);
@@ -1162,12 +1208,12 @@ ts_status ts_init_model(const ts_model_config *cfg, const ts_buffers *bufs, void
   m->tm_qkv.resize(c.n_layers); m->tm_o.resize(c.n_layers); m->tm_gu.resize(c.n_layers); m->tm_d.resize(c.n_layers);
   ts_status s = TS_OK;
   for (int l = 0; l < c.n_layers && !s; ++l) {
-    s = weight_map(enc, &m->tm_qkv[l], m->W(L.wqkv[l]), L.Nqkv, d);
-    if (!s) s = weight_map(enc, &m->tm_o[l], m->W(L.wo[l]), d, Nq);
-    if (!s) s = weight_map(enc, &m->tm_gu[l], m->W(L.wgu[l]), 2 * F, d);
-    if (!s) s = weight_map(enc, &m->tm_d[l], m->W(L.wd[l]), d, F);
+    s = weight_map(enc, c, &m->tm_qkv[l], m->W(L.wqkv[l]), L.Nqkv, d);
+    if (!s) s = weight_map(enc, c, &m->tm_o[l], m->W(L.wo[l]), d, Nq);
+    if (!s) s = weight_map(enc, c, &m->tm_gu[l], m->W(L.wgu[l]), 2 * F, d);
+    if (!s) s = weight_map(enc, c, &m->tm_d[l], m->W(L.wd[l]), d, F);
   }
-  if (!s) s = weight_map(enc, &m->tm_lm, m->W(L.lm_head), c.vocab, d);
+  if (!s) s = weight_map(enc, c, &m->tm_lm, m->W(L.lm_head), c.vocab, d);
   if (!s) s = act_maps(enc, m->tm_h, m->WS(L.h), d, L.rows_alloc, m->planes);
   if (!s) s = act_maps(enc, m->tm_attn, m->WS(L.attn), Nq, L.rows_alloc, m->planes);
   if (!s) s = act_maps(enc, m->tm_act, m->WS(L.act), F, L.rows_alloc, m->planes);
@@ -1245,17 +1291,24 @@ ts_status ts_model_destroy(ts_model *m) {
   return TS_OK;
 }
 
-ts_status ts_load_tensor(ts_model *m, int32_t kind, int32_t layer, const void *host, int64_t rows, int64_t cols) {
-  if (!m || !host) return fail(TS_ERR_ARG, "null argument");
+namespace {
+// Where a tensor belongs: its expected shape, bytes per element, place, and how its rows are dealt out there.
+struct TensorPlace {
+  int64_t er = 0, ec = 0;
+  uint8_t *dst = nullptr;
+  size_t esz = 2;
+  ts::RowMap rm{0, 1, 0, 0};
+};
+ts_status tensor_place(ts_model *m, int32_t kind, int32_t layer, int64_t rows, int64_t cols, TensorPlace *out) {
   const ts_model_config &c = m->c;
   const Layout &L = m->L;
   const int64_t d = c.d_model, F = c.d_ffn, hd = c.head_dim, Nq = (int64_t)c.n_q_heads * hd, Nkv = (int64_t)c.n_kv_heads * hd;
   const bool global = kind == TS_W_EMBED || kind == TS_W_LM_HEAD || kind == TS_W_FINAL_GAIN;
   if (!global && (layer < 0 || layer >= c.n_layers)) return fail(TS_ERR_ARG, "layer %d out of range", layer);
-  int64_t er = 0, ec = 0;
-  uint8_t *dst = nullptr;
-  size_t esz = 2;
-  ts::RowMap rm{0, 1, 0, 0};
+  int64_t &er = out->er, &ec = out->ec;
+  uint8_t *&dst = out->dst;
+  size_t &esz = out->esz;
+  ts::RowMap &rm = out->rm;
   switch (kind) {
     case TS_W_EMBED: er = c.vocab; ec = d; dst = m->W(L.embed); break;
     case TS_W_LM_HEAD: er = c.vocab; ec = d; dst = m->W(L.lm_head); rm.tiles = (c.vocab + 127) / 128; break;
@@ -1273,6 +1326,32 @@ ts_status ts_load_tensor(ts_model *m, int32_t kind, int32_t layer, const void *h
   }
   if (rows != er || cols != ec) return fail(TS_ERR_ARG, "tensor kind %d: expected %lld x %lld, got %lld x %lld", kind,
                                             (long long)er, (long long)ec, (long long)rows, (long long)cols);
+  return TS_OK;
+}
+
+// Stores rows [r0, r0 + nr) of a quantised matrix (device, nb MX blocks a row).
+cudaError_t store_mx(ts_model *m, const TensorPlace &t, const uint8_t *codes, const uint8_t *scales, int64_t nr, int64_t r0, int64_t nb) {
+  return ts::launch_mx_lay_out(codes, scales, (int)nr, (int)r0, (int)nb, t.rm, t.dst, m->st);
+}
+bool on_device(const void *p) {
+  cudaPointerAttributes pa{};
+  const bool yes = cudaPointerGetAttributes(&pa, p) == cudaSuccess && pa.type == cudaMemoryTypeDevice;
+  cudaGetLastError();
+  return yes;
+}
+}  // namespace
+
+ts_status ts_load_tensor(ts_model *m, int32_t kind, int32_t layer, const void *host, int64_t rows, int64_t cols) {
+  if (!m || !host) return fail(TS_ERR_ARG, "null argument");
+  TensorPlace t;
+  ts_status ps = tensor_place(m, kind, layer, rows, cols, &t);
+  if (ps) return ps;
+  const ts_model_config &c = m->c;
+  const Layout &L = m->L;
+  const int64_t er = t.er, ec = t.ec;
+  uint8_t *dst = t.dst;
+  const size_t esz = t.esz;
+  const ts::RowMap rm = t.rm;
   const size_t row_bytes = (size_t)ec * esz;
   if (esz == 4 || kind == TS_W_EMBED) {   // gains and the embedding table stay row-major
     CU_TRY(cudaMemcpyAsync(dst, host, row_bytes * (size_t)er, cudaMemcpyDefault, m->st));
@@ -1282,15 +1361,34 @@ ts_status ts_load_tensor(ts_model *m, int32_t kind, int32_t layer, const void *h
   // Projection matrices: rows go to their place in the stored matrix (Q, K, V concatenated, with rotary
   // partners i and i + hd/2 on adjacent rows 2i and 2i+1; gate and up rows interleaved) and the matrix is
   // stored as 128 x 64 blocks.  Host sources pass through a staging area inside the workspace.
-  cudaPointerAttributes pa{};
-  const bool on_device = cudaPointerGetAttributes(&pa, host) == cudaSuccess && pa.type == cudaMemoryTypeDevice;
-  cudaGetLastError();
+  const bool dev_src = on_device(host);
   const size_t stage_bytes = (size_t)L.step_rows_alloc * (size_t)c.vocab * 4;   // the logits area doubles as staging
-  const int64_t rows_per_chunk = on_device ? er : std::max<int64_t>(1, (int64_t)(stage_bytes / row_bytes));
+  if (c.weights == TS_WEIGHTS_MXFP4) {
+    // quantised on the device, a chunk of rows at a time: codes, scales and, from the host, the rows themselves in the staging area
+    const int64_t nb = (ec + ts::kMxBlock - 1) / ts::kMxBlock;
+    const int64_t per = std::max<int64_t>(1, (int64_t)((stage_bytes - 64) / (17 * (size_t)nb + (dev_src ? 0 : row_bytes))));
+    uint8_t *stage = m->WS(L.logits);
+    for (int64_t r0 = 0; r0 < er; r0 += per) {
+      const int64_t nr = std::min(per, er - r0);
+      uint8_t *codes = stage, *scales = stage + 16 * nb * nr;
+      const void *src = (const uint8_t *)host + (size_t)r0 * row_bytes;
+      if (!dev_src) {
+        void *at = stage + align_up(17 * nb * nr, 32);
+        CU_TRY(cudaMemcpyAsync(at, src, (size_t)nr * row_bytes, cudaMemcpyHostToDevice, m->st));
+        src = at;
+      }
+      CU_TRY(ts::launch_mx_quantise(src, ts::MX_BF16, (int)nr, (int)ec, ec, codes, scales, m->st));
+      CU_TRY(store_mx(m, t, codes, scales, nr, r0, nb));
+      CU_TRY(cudaStreamSynchronize(m->st));
+    }
+    m->have_step = false;
+    return TS_OK;
+  }
+  const int64_t rows_per_chunk = dev_src ? er : std::max<int64_t>(1, (int64_t)(stage_bytes / row_bytes));
   for (int64_t r0 = 0; r0 < er; r0 += rows_per_chunk) {
     const int64_t nr = std::min(rows_per_chunk, er - r0);
     const void *src = (const uint8_t *)host + (size_t)r0 * row_bytes;
-    if (!on_device) {
+    if (!dev_src) {
       CU_TRY(cudaMemcpyAsync(m->WS(L.logits), src, (size_t)nr * row_bytes, cudaMemcpyHostToDevice, m->st));
       src = m->WS(L.logits);
     }
@@ -1298,6 +1396,28 @@ ts_status ts_load_tensor(ts_model *m, int32_t kind, int32_t layer, const void *h
     CU_TRY(cudaStreamSynchronize(m->st));
   }
   m->have_step = false;   // the staging area held the last step's logits
+  return TS_OK;
+}
+
+ts_status ts_load_tensor_mxfp4(ts_model *m, int32_t kind, int32_t layer, const void *codes, const void *scales, int64_t rows, int64_t cols) {
+  if (!m || !codes || !scales) return fail(TS_ERR_ARG, "null argument");
+  if (m->c.weights != TS_WEIGHTS_MXFP4) return fail(TS_ERR_STATE, "the model's weights are not in MXFP4");
+  TensorPlace t;
+  ts_status ps = tensor_place(m, kind, layer, rows, cols, &t);
+  if (ps) return ps;
+  if (t.esz == 4 || kind == TS_W_EMBED) return fail(TS_ERR_ARG, "tensor kind %d is not a projection matrix: ts_load_tensor takes it", kind);
+  const int64_t nb = (t.ec + ts::kMxBlock - 1) / ts::kMxBlock;
+  const size_t stage_bytes = (size_t)m->L.step_rows_alloc * (size_t)m->c.vocab * 4;
+  const int64_t per = std::max<int64_t>(1, (int64_t)(stage_bytes / (17 * (size_t)nb)));
+  uint8_t *stage = m->WS(m->L.logits);
+  for (int64_t r0 = 0; r0 < t.er; r0 += per) {   // (through the staging area wherever they come from: no alignment is asked of them)
+    const int64_t nr = std::min(per, t.er - r0);
+    CU_TRY(cudaMemcpyAsync(stage, (const uint8_t *)codes + r0 * 16 * nb, (size_t)(16 * nb * nr), cudaMemcpyDefault, m->st));
+    CU_TRY(cudaMemcpyAsync(stage + 16 * nb * nr, (const uint8_t *)scales + r0 * nb, (size_t)(nb * nr), cudaMemcpyDefault, m->st));
+    CU_TRY(store_mx(m, t, stage, stage + 16 * nb * nr, nr, r0, nb));
+    CU_TRY(cudaStreamSynchronize(m->st));
+  }
+  m->have_step = false;
   return TS_OK;
 }
 

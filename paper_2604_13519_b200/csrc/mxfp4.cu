@@ -66,7 +66,9 @@ mx_quantise_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols
   for (int i = 0; i < kConvUnroll; ++i) {
     at[i] = pl.at(i * kConvThreads + threadIdx.x);
     if (at[i].row < rows) {
-      mx_load8<TYPE>(x + at[i].row * ldx, true, at[i].col, cols, VEC, v[i]);
+      MxRaw8<TYPE> x8;
+      mx_fetch8<TYPE>(x + at[i].row * ldx, 0, true, at[i].col, cols, VEC, x8);
+      mx_widen8<TYPE>(x8, v[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
@@ -152,25 +154,27 @@ mx_lay_out_kernel(const uint4 *codes, const uint8_t *scales, int n_rows, int n_f
   blk[mx_scale_at(row & 127) + (b & 3)] = there ? scales[(size_t)i * nb + b] : 0;
 }
 
+// The activations of a product as planes, eight elements per thread.  Clears n_flags words at `flags`.
 template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(kConvThreads)
-mx_planes8_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols, long long ldx, uint8_t *out, int ldo, int Mc, int planes,
-                  int *flags, int n_flags) {
+mx_planes8_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols, long long ldx, long long pair, uint8_t *out, int ldo, int Mc,
+                  int planes, int *flags, int n_flags) {
   pdl_launch_dependents();   // (the product waits for this kernel's end before it reads activations)
-  pdl_wait();                // (x may come from the kernel before, whose activations may be in the same workspace)
+  pdl_wait();                // (x may come from the kernel before, whose activations may be in the same scratch memory)
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < n_flags; i += kConvThreads) flags[i] = 0;
   const long long i = (long long)blockIdx.x * kConvThreads + threadIdx.x;
   const int per = ldo / 8;
   const long long row = i / per;
   const int col = (int)(i - row * per) * 8;
+  MxRaw8<TYPE> x8;
   float v[8];
-  mx_load8<TYPE>(x + row * ldx, row < rows, col, cols, VEC, v);
+  mx_fetch8<TYPE>(x + row * ldx, pair, row < rows, col, cols, VEC, x8);
+  mx_widen8<TYPE>(x8, v);
   const int z = (int)(row / Mc), m = (int)(row - (long long)z * Mc), ncols = planes * Mc;
   mx_to_planes(v, row < rows, out + ((size_t)z * (ldo >> 7) + (col >> 7)) * mx_x_block(ncols), ncols * kMxTileK, Mc, planes, m, col & 127);
 }
 
-bool aligned(const void *p, long long ld, int size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
 unsigned conv_blocks(long long rows, int per_row) {
   return (unsigned)((rows * per_row + kConvThreads * kConvUnroll - 1) / (kConvThreads * kConvUnroll));
 }
@@ -187,7 +191,7 @@ unsigned conv_blocks(long long rows, int per_row) {
 cudaError_t launch_mx_quantise(const void *x, int type, int rows, int cols, long long ldx, uint8_t *codes, uint8_t *scales, cudaStream_t st) {
   const int nb = (cols + kMxBlock - 1) / kMxBlock;
   if (rows <= 0 || cols <= 0) return cudaSuccess;
-  const bool vec = aligned(x, ldx, type == MX_F32 ? 4 : 2);
+  const bool vec = mx_aligned(x, ldx, type);
 #define F(T, V) mx_quantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const MxElem<T>::raw *)x, rows, cols, ldx, nb, (uint32_t *)codes, scales)
   MX_BY_TYPE(type, vec, F)
 #undef F
@@ -198,7 +202,7 @@ cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, in
                                  cudaStream_t st) {
   const int nb = (cols + kMxBlock - 1) / kMxBlock;
   if (rows <= 0 || cols <= 0) return cudaSuccess;
-  const bool vec = aligned(y, ldy, type == MX_F32 ? 4 : 2);
+  const bool vec = mx_aligned(y, ldy, type);
 #define F(T, V) mx_dequantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const uint32_t *)codes, scales, rows, cols, nb, (MxElem<T>::raw *)y, ldy)
   MX_BY_TYPE(type, vec, F)
 #undef F
@@ -216,11 +220,10 @@ cudaError_t launch_mx_lay_out(const uint8_t *codes, const uint8_t *scales, int n
 }
 
 template <int TYPE, bool VEC>
-static cudaError_t planes8(const void *x, int rows, int cols, long long ldx, uint8_t *out, int Mc, int planes, int *flags, int n_flags,
-                           cudaStream_t st, bool pdl) {
-  const int ldo = (cols + 127) / 128 * 128;
+static cudaError_t planes8(const MxInput &in, uint8_t *out, int Mc, int *flags, int n_flags, cudaStream_t st, bool pdl) {
+  const int ldo = (in.cols + kMxTileK - 1) / kMxTileK * kMxTileK;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(((long long)rows * (ldo / 8) + kConvThreads - 1) / kConvThreads));
+  cfg.gridDim = dim3((unsigned)(((long long)in.rows * (ldo / 8) + kConvThreads - 1) / kConvThreads));
   cfg.blockDim = dim3(kConvThreads);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -228,15 +231,30 @@ static cudaError_t planes8(const void *x, int rows, int cols, long long ldx, uin
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = pdl ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, mx_planes8_kernel<TYPE, VEC>, (const typename MxElem<TYPE>::raw *)x, (long long)rows, cols, ldx, out, ldo, Mc, planes,
-                            flags, n_flags);
+  return cudaLaunchKernelEx(&cfg, mx_planes8_kernel<TYPE, VEC>, (const typename MxElem<TYPE>::raw *)in.x, (long long)in.rows, in.cols, in.ldx, in.pair,
+                            out, ldo, Mc, mx_planes_of(TYPE), flags, n_flags);
 }
-cudaError_t launch_mx_planes8(const void *x, int type, int rows, int cols, long long ldx, uint8_t *out, int Mc, int planes, int *flags, int n_flags,
-                              cudaStream_t st, bool pdl) {
-  const bool vec = aligned(x, ldx, type == MX_F32 ? 4 : 2);
-#define F(T, V) return planes8<T, V>(x, rows, cols, ldx, out, Mc, planes, flags, n_flags, st, pdl)
-  MX_BY_TYPE(type, vec, F)
+cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st, bool pdl) {
+  const MxScratch w = mx_scratch((in.cols + kMxTileK - 1) / kMxTileK, mx_planes_of(in.type), p);
+  uint8_t *out = (uint8_t *)scratch;
+  int *flags = (int *)(out + w.flags);
+  const int n_flags = p.stream ? p.chunks * p.ctas : 0;
+  const bool vec = mx_aligned(in.x, in.ldx, in.type) && (in.type != MX_PAIR || in.pair % 8 == 0);
+  if (in.type == MX_PAIR) return vec ? planes8<MX_PAIR, true>(in, out, p.Mc, flags, n_flags, st, pdl) : planes8<MX_PAIR, false>(in, out, p.Mc, flags, n_flags, st, pdl);
+#define F(T, V) return planes8<T, V>(in, out, p.Mc, flags, n_flags, st, pdl)
+  MX_BY_TYPE(in.type, vec, F)
 #undef F
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+int mx_weight_map(void *encode, CUtensorMap *map, const void *data, uint64_t blocks) {
+  const cuuint64_t dims[3] = {kMxTileK, kMxTileN, blocks}, strides[2] = {kMxTileK / 2, kMxTileBytes};
+  const cuuint32_t box[3] = {kMxTileK, kMxTileN, 1}, es[3] = {1, 1, 1};
+  return (int)((EncodeTiledFn)encode)(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 3, const_cast<void *>(data), dims, strides, box, es,
+                                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 }  // namespace ts
@@ -248,9 +266,7 @@ using ts::set_error;
 
 constexpr int64_t kMostSide = 1 << 21;   // rows and columns of a matrix
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+using ts::EncodeTiledFn;
 
 // What a device offers, asked for once per device.
 struct MxDevice {
@@ -307,22 +323,8 @@ ts_status packed_ok(const void *codes, const void *scales, int64_t rows, int64_t
   if ((uintptr_t)codes % 16) return set_error(TS_ERR_ARG, "codes must be 16-byte aligned");
   return TS_OK;
 }
-int planes_of(int32_t type) { return type == TS_MX_BF16 ? 2 : type == TS_MX_F16 ? 3 : 5; }
 uint64_t tiles_of(int64_t n) { return (uint64_t)(n + ts::kMxTileN - 1) / ts::kMxTileN; }
 uint64_t kblocks_of(int64_t k) { return (uint64_t)(k + ts::kMxTileK - 1) / ts::kMxTileK; }
-
-// What a product keeps in its workspace: the activations' planes, where it is dealt out in runs a flag
-// and a slab of sums for each CTA.
-struct Workspace { uint64_t flags, slabs, bytes; };
-Workspace workspace_of(int64_t k, int planes, const ts::MxPlan &p) {
-  Workspace w;
-  if (p.own) return Workspace{};
-  w.flags = (uint64_t)p.chunks * kblocks_of(k) * ts::mx_x_block(planes * p.Mc);
-  w.slabs = w.flags + (p.stream ? ((uint64_t)p.ctas * 4 + 127) / 128 * 128 : 0);
-  w.bytes = w.slabs + (p.stream ? (uint64_t)p.ctas * p.Mc * ts::kMxTileN * 4 : 0);
-  return w;
-}
-constexpr int kMostSms = 256;   // (the size of a workspace is asked for without a device)
 
 #define MX_TRY(call)                                                                                      \
   do {                                                                                                    \
@@ -391,12 +393,7 @@ ts_status ts_mxfp4_matrix_init(ts_mxfp4_matrix *m, const void *data, int64_t n, 
   MX_OK(device_of_call(&d));
   CUtensorMap map;
   static_assert(sizeof map == sizeof m->map, "a descriptor has 128 bytes");
-  const cuuint64_t dims[3] = {128, 128, (cuuint64_t)(tiles_of(n) * kblocks_of(k))};
-  const cuuint64_t strides[2] = {64, ts::kMxTileBytes};
-  const cuuint32_t box[3] = {128, 128, 1}, es[3] = {1, 1, 1};
-  const CUresult r = g_encode.load(std::memory_order_acquire)(&map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 3, const_cast<void *>(data), dims, strides,
-                                                              box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                                              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const CUresult r = (CUresult)ts::mx_weight_map((void *)g_encode.load(std::memory_order_acquire), &map, data, tiles_of(n) * kblocks_of(k));
   if (r != CUDA_SUCCESS) return set_error(TS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
   m->data = data;
   std::memcpy(m->map, &map, sizeof map);
@@ -409,18 +406,7 @@ ts_status ts_mxfp4_product_workspace(int64_t rows, int64_t n, int64_t k, int32_t
   MX_OK(matrix_ok(rows, k));
   if (!type_ok(x_type)) return set_error(TS_ERR_ARG, "unknown element type %d", x_type);
   *bytes = 0;
-  if (rows && n && k) {
-    // Enough for fewer rows too, and whatever the device's number of SMs: as many flags and slabs as there may be, chunks counted at their
-    // largest.
-    const int planes = planes_of(x_type), tiles = (int)tiles_of(n), n_kb = (int)kblocks_of(k);
-    ts::MxPlan p = ts::mx_plan((int)rows, tiles, n_kb, planes, 1);
-    const ts::MxPlan full = ts::mx_plan(1 << 20, 1, 1, planes, 1);
-    if (p.chunks > 1) p.Mc = full.Mc;
-    p.own = false;
-    p.stream = true;
-    p.ctas = 2 * kMostSms;
-    *bytes = workspace_of(k, planes, p).bytes;
-  }
+  if (n) *bytes = ts::mx_scratch_most((int)rows, (int)kblocks_of(k), ts::mx_planes_of(x_type));
   return TS_OK;
 }
 
@@ -443,31 +429,24 @@ ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
   }
   if (!w->data) return set_error(TS_ERR_ARG, "the matrix has no data");
 
-  const int planes = planes_of(a->x_type);
-  const ts::MxPlan p = ts::mx_plan((int)M, (int)tiles_of(N), (int)kblocks_of(K), planes, std::min(d.sms, kMostSms));
-  const Workspace ws = workspace_of(K, planes, p);
-  if (ws.bytes && (!a->workspace || a->workspace_bytes < ws.bytes || (uintptr_t)a->workspace % 128))
-    return set_error(TS_ERR_ARG, "workspace of %llu bytes, 128-byte aligned, needed for these rows", (unsigned long long)ws.bytes);
   ts::MxArgs g{};
   g.w = (const uint8_t *)w->data;
-  g.N = (int)N; g.M = (int)M;
+  g.N = (int)N;
   g.tiles = (int)tiles_of(N); g.n_kb = (int)kblocks_of(K);
-  g.planes = planes;
   g.err = a->status;
   g.y = a->y; g.ldy = a->ldy; g.y_type = a->y_type;
   const size_t ysz = type_size(a->y_type);
   g.vec = a->ldy % 4 == 0 && (uintptr_t)a->y % (4 * ysz) == 0;
-  uint8_t *base = (uint8_t *)a->workspace;
-  g.x = p.own ? a->x : base;
-  g.ldx = a->ldx; g.x_type = a->x_type; g.K = (int)K;
-  g.vec_x = ts::aligned(a->x, a->ldx, (int)type_size(a->x_type));
-  g.flags = (int *)(base + ws.flags);
-  g.slabs = (float *)(base + ws.slabs);
-  if (!p.own)
-    MX_TRY(ts::launch_mx_planes8(a->x, a->x_type, (int)M, (int)K, a->ldx, base, p.Mc, planes, g.flags, p.stream ? p.ctas : 0, st, true));
+  const ts::MxInput in{a->x, a->x_type, (int)M, (int)K, a->ldx, 0};
+  const int planes = ts::mx_planes_of(a->x_type);
+  const ts::MxPlan p = ts::mx_plan((int)M, g.tiles, g.n_kb, planes, d.sms);
+  const uint64_t need = ts::mx_scratch(g.n_kb, planes, p).bytes;
+  if (need && (!a->workspace || a->workspace_bytes < need || (uintptr_t)a->workspace % 128))
+    return set_error(TS_ERR_ARG, "workspace of %llu bytes, 128-byte aligned, needed for these rows", (unsigned long long)need);
+  if (!p.own) MX_TRY(ts::launch_mx_input(in, a->workspace, p, st, true));
   CUtensorMap tw;
   std::memcpy(&tw, w->map, sizeof tw);
-  MX_TRY(ts::launch_mx_product(ts::MX_STORE, tw, g, p, st, true));
+  MX_TRY(ts::launch_mx_product(ts::MX_STORE, tw, g, in, a->workspace, p, st, true, nullptr));
   return TS_OK;
 }
 

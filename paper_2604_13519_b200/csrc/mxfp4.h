@@ -17,16 +17,18 @@ __host__ __device__ inline int mx_scale_at(int row) { return kMxCodeBytes + (row
 
 __host__ __device__ inline int mx_block(int tile, int kb, int n_kb) { return tile * n_kb + kb; }
 
-enum : int { MX_BF16 = 0, MX_F16 = 1, MX_F32 = 2 };   // element types of activations and results (TS_MX_*)
+// Element types of activations and results (TS_MX_*); MX_PAIR, a model's activations: two arrays of bf16 whose sum is meant.
+enum : int { MX_BF16 = 0, MX_F16 = 1, MX_F32 = 2, MX_PAIR = 3 };
+inline int mx_planes_of(int type) { return type == MX_BF16 ? 2 : type == MX_F16 ? 3 : type == MX_F32 ? 5 : 4; }
 
 struct MxArgs {
   const uint8_t *w;          // laid-out matrix
   const void *x;             // the activations' planes, see launch_mx_planes8; with plan.own the rows themselves:
-  long long ldx;             // row stride
+  long long ldx, pair;       // row stride; MX_PAIR: distance of the two arrays, in elements
   int x_type, vec_x, K;      // type, rows can be read 16 bytes at a time, columns
   float *slabs;              // [CTA][Mc][128] sums of tiles that the CTA has without their last k-blocks
   int *flags;                // [CTA] its slab is there (zero before the launch)
-  int N, M;                  // features, activation rows
+  int N, M, row0;            // features, activation rows of this launch, the first one's place among all rows of the result
   int tiles, n_kb;           // 128-row tiles and 128-column blocks of the matrix
   int planes;                // planes of e4m3 numbers that are added
   int Mc, chunks, stages, n_acc;   // filled in by the launcher: activation rows per tile of the result, their chunks, stages of the ring, accumulators
@@ -51,8 +53,9 @@ template <int TYPE> struct MxElem;
 template <> struct MxElem<MX_BF16> { typedef uint16_t raw; };
 template <> struct MxElem<MX_F16> { typedef uint16_t raw; };
 template <> struct MxElem<MX_F32> { typedef uint32_t raw; };
+template <> struct MxElem<MX_PAIR> { typedef uint16_t raw; };
 template <int TYPE> __device__ __forceinline__ float mx_to_f32(typename MxElem<TYPE>::raw r) {
-  if constexpr (TYPE == MX_BF16) return __uint_as_float((uint32_t)r << 16);
+  if constexpr (TYPE == MX_BF16 || TYPE == MX_PAIR) return __uint_as_float((uint32_t)r << 16);
   else if constexpr (TYPE == MX_F16) return __half2float(__ushort_as_half(r));
   else return __uint_as_float(r);
 }
@@ -63,26 +66,28 @@ template <int TYPE> __device__ __forceinline__ typename MxElem<TYPE>::raw mx_fro
 }
 
 // elements [c, c + 8) of a row of `cols` as they are, zeros behind its end and where `there` is false
-template <int TYPE> struct MxRaw8 { __align__(16) typename MxElem<TYPE>::raw r[8]; };
+template <int TYPE> struct MxRaw8 { __align__(16) typename MxElem<TYPE>::raw r[TYPE == MX_PAIR ? 16 : 8]; };
 template <int TYPE>
-__device__ __forceinline__ void mx_fetch8(const typename MxElem<TYPE>::raw *p, bool there, int c, int cols, bool vec, MxRaw8<TYPE> &x) {
-  if (vec && there && c + 8 <= cols) {
+__device__ __forceinline__ void mx_fetch8(const typename MxElem<TYPE>::raw *p, long long pair, bool there, int c, int cols, bool vec, MxRaw8<TYPE> &x) {
+  constexpr int kArrays = TYPE == MX_PAIR ? 2 : 1;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(x.r[0]) / 2; ++i) reinterpret_cast<uint4 *>(x.r)[i] = __ldg(reinterpret_cast<const uint4 *>(p + c) + i);
-  } else {
+  for (int h = 0; h < kArrays; ++h) {
+    const typename MxElem<TYPE>::raw *q = p + h * pair;
+    if (vec && there && c + 8 <= cols) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x.r[i] = there && c + i < cols ? p[c + i] : 0;
+      for (int i = 0; i < (int)sizeof(x.r[0]) / 2; ++i) reinterpret_cast<uint4 *>(x.r + 8 * h)[i] = __ldg(reinterpret_cast<const uint4 *>(q + c) + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x.r[8 * h + i] = there && c + i < cols ? q[c + i] : 0;
+    }
   }
 }
 template <int TYPE> __device__ __forceinline__ void mx_widen8(const MxRaw8<TYPE> &x, float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = mx_to_f32<TYPE>(x.r[i]);
-}
-template <int TYPE>
-__device__ __forceinline__ void mx_load8(const typename MxElem<TYPE>::raw *p, bool there, int c, int cols, bool vec, float (&v)[8]) {
-  MxRaw8<TYPE> x;
-  mx_fetch8<TYPE>(p, there, c, cols, vec, x);
-  mx_widen8<TYPE>(x, v);
+  for (int i = 0; i < 8; ++i) {
+    v[i] = mx_to_f32<TYPE>(x.r[i]);
+    if constexpr (TYPE == MX_PAIR) v[i] += mx_to_f32<TYPE>(x.r[8 + i]);   // (exact: the second is the rounding remainder of the first)
+  }
 }
 
 // Eight elements at columns col .. col + 7 of row m (m: within its chunk) into the planes of a block of 128 columns (col: within it) at
@@ -179,12 +184,30 @@ template <int EPI> __device__ __forceinline__ void mx_finish(const MxArgs &g, lo
 }
 #endif
 
-// How a product is dealt out: activation rows per chunk (a multiple of 8, planes x rows one of 16), chunks; runs of k-blocks (stream) or
-// a tile to each of `ctas` clusters; whether it makes the planes itself.
-struct MxPlan { int Mc, chunks, ctas, cluster; bool stream, own; };
+// How a product is dealt out: activation rows per chunk (a multiple of 8, planes x rows one of 16), chunks, and whether each of them is
+// a launch of its own; runs of k-blocks (stream) or a tile to each of `ctas` clusters; whether it makes the planes itself.
+struct MxPlan { int Mc, chunks, ctas, cluster; bool apart, stream, own; };
 MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms);
+
+// Activations, and the scratch memory of a product with them: planes, and for products dealt out in runs flags and slabs.
+struct MxInput {
+  const void *x;
+  int type, rows, cols;
+  long long ldx, pair;   // (see MxArgs)
+};
+struct MxScratch { uint64_t flags, slabs, bytes; };
+MxScratch mx_scratch(int n_kb, int planes, const MxPlan &p);
+// Enough for products with matrices of `n_kb` k-blocks or fewer with up to `rows` rows, whatever their features and the device.
+uint64_t mx_scratch_most(int rows, int n_kb, int planes);
+constexpr int kMxMostSms = 256;
+// whether rows of 16- or 32-bit elements can be read 16 bytes at a time
+inline bool mx_aligned(const void *p, long long ld, int type) { return ((uintptr_t)p & 15) == 0 && ld * (type == MX_F32 ? 4 : 2) % 16 == 0; }
+
 // `tw`: the matrix's elements, blocks of 128 x 128, widened to bytes by the copy, 128-byte swizzle.
-cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxPlan &p, cudaStream_t st, bool pdl);
+// Before it, unless the plan says `own`, launch_mx_input.  `g` holds the matrix, err, stamp and the outputs; launches: how many.
+cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st,
+                              bool pdl, int *launches);
+cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st, bool pdl);
 // bytes of 128 columns of the activations with `ncols` = planes x Mc instruction columns: elements, then scales
 __host__ __device__ inline int mx_x_block(int ncols) { return ncols * kMxTileK + 512 * ((ncols + 127) / 128); }
 
@@ -194,11 +217,11 @@ cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, in
 // Rows [r0, r0 + n_rows) of a quantised matrix with nb MX blocks a row (codes, scales: the first of these rows) into the blocks of
 // the laid-out matrix (rm as for launch_retile).
 cudaError_t launch_mx_lay_out(const uint8_t *codes, const uint8_t *scales, int n_rows, int r0, int nb, RowMap rm, uint8_t *w, cudaStream_t st);
-// x [rows][cols] (row stride ldx) as planes of e4m3 numbers, in blocks as the product's shared memory holds them: [chunk of Mc rows]
-// [128 columns] { elements [column c of the instruction = plane * Mc + row][128 bytes, 16-byte pieces swizzled: piece ^ (c & 7)],
-// scales [c / 128][lane c % 32][word c / 32 % 4][4 bytes, one per MX block] }.  Rows behind the last one of a chunk stay as they are.
-// Clears n_flags words at `flags`.
-cudaError_t launch_mx_planes8(const void *x, int type, int rows, int cols, long long ldx, uint8_t *out, int Mc, int planes, int *flags, int n_flags,
-                              cudaStream_t st, bool pdl);
+// The descriptor of a laid-out matrix of `blocks` blocks (encode: cuTensorMapEncodeTiled); returns a CUresult.
+int mx_weight_map(void *encode, CUtensorMap *map, const void *data, uint64_t blocks);
+
+// Planes (mx_planes8_kernel) lie in blocks as the product's shared memory holds them: [chunk of Mc rows][128 columns] { elements [column c
+// of the instruction = plane * Mc + row][128 bytes, 16-byte pieces swizzled: piece ^ (c & 7)], scales [c / 128][lane c % 32]
+// [word c / 32 % 4][4 bytes, one per MX block] }.  Rows behind the last one of a chunk stay as they are.
 
 }  // namespace ts

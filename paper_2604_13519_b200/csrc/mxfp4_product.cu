@@ -356,7 +356,7 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
             }
             w[0] += sum.x; w[1] += sum.y; w[2] += sum.z; w[3] += sum.w;
           }
-          mx_finish<EPI>(g, m0 + c0 + i, n, w, lane);
+          mx_finish<EPI>(g, g.row0 + m0 + c0 + i, n, w, lane);
         }
       }
       if (!whole) {
@@ -408,7 +408,7 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
         for (int c = 0; c < 8; ++c)
           if (c < C) { v[0] += p[c].x; v[1] += p[c].y; v[2] += p[c].z; v[3] += p[c].w; }
       }
-      mx_finish<EPI>(g, m0 + m, n, v, lane);
+      mx_finish<EPI>(g, g.row0 + m0 + m, n, v, lane);
     }
   } else if (kOwn) {
     // ------------------------------------------------------------------ planes
@@ -423,14 +423,14 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
     MxRaw8<TYPE> x[kAhead];
     int i = warp - 6;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) mx_fetch8<TYPE>(row, there && i + j * kWarps < nkb, (kb0 + i + j * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
+    for (int j = 0; j < kAhead; ++j) mx_fetch8<TYPE>(row, g.pair, there && i + j * kWarps < nkb, (kb0 + i + j * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
     for (bool ok = true; ok && i < nkb;) {
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         if (!ok || i >= nkb) break;
         float v[8];
         mx_widen8<TYPE>(x[j], v);
-        mx_fetch8<TYPE>(row, there && i + kAhead * kWarps < nkb, (kb0 + i + kAhead * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
+        mx_fetch8<TYPE>(row, g.pair, there && i + kAhead * kWarps < nkb, (kb0 + i + kAhead * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
         const int s = i % g.stages;
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->empty[s]), ((i / g.stages) & 1) ^ 1));
         if (!ok) {
@@ -473,20 +473,42 @@ static size_t prod_stage_bytes(int planes, int Mc) {
 }
 
 // Rows per chunk: all of them up to 224 instruction columns, else equal chunks of fewer.  Then CTAs, two to an SM: runs of k-blocks where
-// there are more tiles than places, else clusters of as many as there is room for, eight at most.
-constexpr int kOwnRows = 2;   // most rows whose planes the product makes itself
+// there are more tiles than places, else clusters of as many as there is room for, eight at most.  Up to 64 rows neither the cut along K nor
+// the order of the sums may depend on the number of rows: chunks are then launches of their own.
+constexpr int kOwnRows = 2;     // most rows whose planes the product makes itself
+constexpr int kSameRows = 64;
 MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms) {
   MxPlan p{};
   const int step = planes % 2 ? 16 : 8, most = kProdAcc / planes / step * step;   // (the instruction's N, planes x rows, is a multiple of 16)
   p.chunks = (M + most - 1) / most;
   p.Mc = ((M + p.chunks - 1) / p.chunks + step - 1) / step * step;
   p.chunks = (M + p.Mc - 1) / p.Mc;
-  const long long items = (long long)tiles * p.chunks, places = (long long)kProdCtas * n_sms;
-  p.stream = items > places && p.chunks == 1;
+  p.apart = M <= kSameRows;
+  const long long items = (long long)tiles * (p.apart ? 1 : p.chunks), places = (long long)kProdCtas * std::min(n_sms, kMxMostSms);
+  p.stream = items > places && (p.apart || p.chunks == 1);
   p.cluster = p.stream ? 1 : (int)std::max<long long>(1, std::min<long long>(std::min(8, n_kb), places / items));
   p.ctas = (int)(p.stream ? places : items);
   p.own = !p.stream && M <= kOwnRows;
   return p;
+}
+
+MxScratch mx_scratch(int n_kb, int planes, const MxPlan &p) {
+  MxScratch w{};
+  if (p.own) return w;
+  const uint64_t n_flags = p.stream ? (uint64_t)p.chunks * p.ctas : 0;   // (a launch's flags are its own, the slabs are reused)
+  w.flags = (uint64_t)p.chunks * n_kb * mx_x_block(planes * p.Mc);
+  w.slabs = w.flags + (n_flags * 4 + 127) / 128 * 128;
+  w.bytes = w.slabs + (p.stream ? (uint64_t)p.ctas * p.Mc * kMxTileN * 4 : 0);
+  return w;
+}
+uint64_t mx_scratch_most(int rows, int n_kb, int planes) {
+  if (!rows || !n_kb) return 0;
+  MxPlan p = mx_plan(rows, 1, n_kb, planes, 1);
+  if (p.chunks > 1) p.Mc = mx_plan(1 << 20, 1, 1, planes, 1).Mc;   // (equal chunks may be larger for fewer rows)
+  p.own = false;
+  p.stream = true;
+  p.ctas = kProdCtas * kMxMostSms;
+  return mx_scratch(n_kb, planes, p).bytes;
 }
 
 template <int EPI, bool kStream, bool kOwn, int TYPE>
@@ -529,28 +551,46 @@ static cudaError_t prod_launch(const CUtensorMap &tw, const MxArgs &g, const MxP
   switch (g.x_type) {
     case MX_BF16: return prod_launch_one<EPI, false, true, MX_BF16>(tw, g, p, smem, st, pdl);
     case MX_F16: return prod_launch_one<EPI, false, true, MX_F16>(tw, g, p, smem, st, pdl);
+    case MX_PAIR: return prod_launch_one<EPI, false, true, MX_PAIR>(tw, g, p, smem, st, pdl);
     default: return prod_launch_one<EPI, false, true, MX_F32>(tw, g, p, smem, st, pdl);
   }
 }
 
-cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxPlan &p, cudaStream_t st, bool pdl) {
-  g.Mc = p.Mc; g.chunks = p.chunks;
-  g.units = (long long)g.tiles * g.chunks * g.n_kb;
+cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st,
+                              bool pdl, int *launches) {
+  const MxScratch w = mx_scratch(g.n_kb, mx_planes_of(in.type), p);
+  g.planes = mx_planes_of(in.type);
+  g.Mc = p.Mc;
+  g.ldx = in.ldx; g.pair = in.pair; g.x_type = in.type; g.K = in.cols;
+  g.vec_x = mx_aligned(in.x, in.ldx, in.type) && (in.type != MX_PAIR || in.pair % 8 == 0);
+  g.slabs = (float *)((uint8_t *)scratch + w.slabs);
   const size_t stage = prod_stage_bytes(g.planes, g.Mc), fixed = kProdStaging + sizeof(ProdSmemCtl);
   g.stages = (int)std::min<size_t>(kProdMaxStages, (113 * 1024 - fixed) / stage);
   const int ncols = g.planes * g.Mc;
   const int acc = (ncols + 31) & ~31, sets = g.stages * (4 + 4 * ((ncols + 127) / 128));   // columns of an accumulator, of all scales
   g.n_acc = p.stream && 2 * acc + sets <= 256 ? 2 : 1;
-  if (g.stages < 2 || g.Mc % 8 || ncols % 16 || ncols > kProdAcc || g.n_acc * acc + sets > 256 || p.ctas < 1 || p.cluster < 1 || p.cluster > 8 || p.cluster > g.n_kb ||
-      (p.stream && p.ctas > g.units) || (size_t)g.stages * stage < (size_t)g.Mc * kMxTileN * 4)
-    return cudaErrorInvalidValue;
   const size_t smem = g.stages * stage + fixed;
-  switch (epi) {
-    case MX_STORE: return prod_launch<MX_STORE>(tw, g, p, smem, st, pdl);
-    case MX_SWIGLU: return prod_launch<MX_SWIGLU>(tw, g, p, smem, st, pdl);
-    case MX_LOGITS: return prod_launch<MX_LOGITS>(tw, g, p, smem, st, pdl);
+  const int passes = p.apart ? p.chunks : 1;
+  g.chunks = p.apart ? 1 : p.chunks;
+  g.units = (long long)g.tiles * g.chunks * g.n_kb;
+  if (g.stages < 2 || g.Mc % 8 || ncols % 16 || ncols > kProdAcc || g.n_acc * acc + sets > 256 || p.ctas < 1 || p.cluster < 1 || p.cluster > 8 ||
+      p.cluster > g.n_kb || (p.stream && p.ctas > g.units) || (size_t)g.stages * stage < (size_t)g.Mc * kMxTileN * 4 || (p.own && passes != 1))
+    return cudaErrorInvalidValue;
+  for (int i = 0; i < passes; ++i) {
+    g.row0 = i * g.Mc;
+    g.M = passes == 1 ? in.rows : std::min(g.Mc, in.rows - g.row0);
+    g.x = p.own ? in.x : (const uint8_t *)scratch + (size_t)i * g.n_kb * mx_x_block(ncols);
+    g.flags = (int *)((uint8_t *)scratch + w.flags) + (p.stream ? i * p.ctas : 0);
+    cudaError_t e = cudaErrorInvalidValue;
+    switch (epi) {
+      case MX_STORE: e = prod_launch<MX_STORE>(tw, g, p, smem, st, pdl); break;
+      case MX_SWIGLU: e = prod_launch<MX_SWIGLU>(tw, g, p, smem, st, pdl); break;
+      case MX_LOGITS: e = prod_launch<MX_LOGITS>(tw, g, p, smem, st, pdl); break;
+    }
+    if (e != cudaSuccess) return e;
   }
-  return cudaErrorInvalidValue;
+  if (launches) *launches = passes;
+  return cudaSuccess;
 }
 
 }  // namespace ts

@@ -208,8 +208,6 @@ def test_a_row_s_result_does_not_depend_on_the_others(n, k, x_type):
     _, _, w = _weights(rng, n, k)
     x = torch.randn(64, k, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(TYPES[x_type])
     whole = ts.ts_mxfp4_product(w, x, torch.float32)
-    if x_type == "f32":
-        x, whole = x[:32], ts.ts_mxfp4_product(w, x[:32], torch.float32)
     for m in (1, 2, 7, 8, 9, 16, 17, 31, 33, 40, 48, 63):
         assert torch.equal(ts.ts_mxfp4_product(w, x[:m], torch.float32), whole[:m]), m
     assert torch.equal(ts.ts_mxfp4_product(w, x[13:14].contiguous(), torch.float32), whole[13:14])

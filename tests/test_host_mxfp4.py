@@ -111,3 +111,24 @@ def test_binding_refuses():
         B._mx_type(torch.float64)
     with pytest.raises(ValueError):
         B._mx_packed(torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.uint8), 64)
+
+
+def test_model_configuration_refuses():
+    import synth
+    L, out = B.lib(), B.ts_buffer_sizes()
+    s = synth.SHAPES["8b"]
+    c = B.ts_model_config()
+    for n in ("n_layers", "d_model", "n_q_heads", "n_kv_heads", "head_dim", "d_ffn", "vocab", "rope_theta", "rms_eps"):
+        setattr(c, n, getattr(s, n))
+    c.max_pages, c.max_batch, c.k_max, c.max_rows, c.max_ctx, c.act_split = 1024, 1, 32, 32, 16384, 1
+    assert L.ts_query_buffer_sizes(C.byref(c), C.byref(out)) == 0
+    full, work = out.weights_bytes, out.workspace_bytes
+    c.weights = B.TS_WEIGHTS_MXFP4
+    assert L.ts_query_buffer_sizes(C.byref(c), C.byref(out)) == 0
+    embed = 2 * s.vocab * s.d_model
+    assert abs((out.weights_bytes - embed) / (full - embed) - 17 / 64) < 1e-3 and out.workspace_bytes > work
+    c.path = 2
+    _refused(L.ts_query_buffer_sizes(C.byref(c), C.byref(out)), "path 2")
+    c.path, c.weights = 0, 2
+    _refused(L.ts_query_buffer_sizes(C.byref(c), C.byref(out)), "weights")
+    _refused(L.ts_load_tensor_mxfp4(None, 3, 0, P, P, 4, 64), "null")
