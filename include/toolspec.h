@@ -517,8 +517,8 @@ ts_status ts_mxfp4_matrix_init(ts_mxfp4_matrix *m, const void *data, int64_t n, 
  * The tensor cores multiply the four-bit elements as they are; x goes in as a sum of 2 (bf16), 3 (fp16) or 5 (fp32) numbers of four
  * significant bits with a scale per 32 columns, which leaves out less than 2^-20 of the largest of the 32 (of bf16 and fp16 rows
  * nothing of elements down to 2^-13 of it); sums are fp32.  A row that holds an infinity or a NaN gives NaN.
- * A row's result depends on that row and on the matrix, not on the other rows: with up to 64 rows it is the same, bit for
- * bit, whatever their number.  What lies between the rows of y is left as it is; y must not overlap x or the matrix.
+ * A row's result depends on that row and on the matrix, not on the other rows: with up to 64 rows (fp32: 32) it is the same, bit
+ * for bit, whatever their number.  What lies between the rows of y is left as it is; y must not overlap x or the matrix.
  * workspace: device, 128-byte aligned, of ts_mxfp4_product_workspace bytes (host only call; enough for fewer rows too).  It holds nothing
  * between calls; calls that overlap on the GPU need one each.
  * status: device, one int32, or NULL: takes a value other than 0 if a wait inside the kernel expired (y is then not valid). */

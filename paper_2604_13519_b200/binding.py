@@ -664,14 +664,16 @@ def _mx_rows(t, name):
 
 
 def _mx_packed(codes, scales, cols):
-    import torch
+    """Checks codes and scales of a matrix of `cols` columns; its rows."""
     nb = (cols + 31) // 32
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or scales.device != codes.device:
+    if codes.element_size() != 1 or scales.element_size() != 1 or not codes.is_cuda or scales.device != codes.device:
         raise ValueError("codes and scales must be uint8 tensors on one CUDA device")
-    if codes.dim() != 2 or tuple(codes.shape) != (codes.shape[0], 16 * nb) or tuple(scales.shape) != (codes.shape[0], nb):
+    rows = codes.shape[0]
+    if codes.shape != (rows, 16 * nb) or scales.shape != (rows, nb):
         raise ValueError(f"{cols} columns take codes of [rows][{16 * nb}] and scales of [rows][{nb}]")
     if not codes.is_contiguous() or not scales.is_contiguous():
         raise ValueError("codes and scales must be contiguous")
+    return rows
 
 
 def _on_device_of(index, stream, call, *args):
@@ -691,9 +693,10 @@ def ts_mxfp4_quantise(x, stream=None):
     import torch
     rows, cols, ldx = _mx_rows(x, "x")
     nb = (cols + 31) // 32
-    codes = torch.empty(rows, 16 * nb, dtype=torch.uint8, device=x.device)
-    scales = torch.empty(rows, nb, dtype=torch.uint8, device=x.device)
-    _on_device_of(x.device.index, stream, lib().ts_mxfp4_quantise, x.data_ptr(), _mx_type(x.dtype), rows, cols, ldx, codes.data_ptr(),
+    device = x.device
+    codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=device)
+    scales = torch.empty((rows, nb), dtype=torch.uint8, device=device)
+    _on_device_of(device.index, stream, lib().ts_mxfp4_quantise, x.data_ptr(), _mx_type(x.dtype), rows, cols, ldx, codes.data_ptr(),
                   scales.data_ptr())
     return codes, scales
 
@@ -701,14 +704,16 @@ def ts_mxfp4_quantise(x, stream=None):
 def ts_mxfp4_dequantise(codes, scales, cols: int, dtype, out=None, stream=None):
     """The values of an MXFP4 matrix of `cols` columns, in `dtype` (bf16, fp16, fp32); written into `out` if it is given."""
     import torch
-    _mx_packed(codes, scales, cols)
-    y = torch.empty(codes.shape[0], cols, dtype=dtype, device=codes.device) if out is None else out
-    if y.dtype != dtype or tuple(y.shape) != (codes.shape[0], cols) or y.device != codes.device:
-        raise ValueError("out does not match the matrix")
-    rows, _, ldy = _mx_rows(y, "out")
-    _on_device_of(codes.device.index, stream, lib().ts_mxfp4_dequantise, codes.data_ptr(), scales.data_ptr(), rows, cols, y.data_ptr(),
+    rows = _mx_packed(codes, scales, cols)
+    if out is None:
+        out, ldy = torch.empty((rows, cols), dtype=dtype, device=codes.device), cols
+    else:
+        have, width, ldy = _mx_rows(out, "out")
+        if out.dtype != dtype or (have, width) != (rows, cols) or out.device != codes.device:
+            raise ValueError("out does not match the matrix")
+    _on_device_of(codes.device.index, stream, lib().ts_mxfp4_dequantise, codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(),
                   _mx_type(dtype), ldy)
-    return y
+    return out
 
 
 class Mxfp4Matrix:
@@ -716,8 +721,8 @@ class Mxfp4Matrix:
 
     def __init__(self, codes, scales, k: int, stream=None):
         import torch
-        _mx_packed(codes, scales, k)
-        self.n, self.k, self.device, self.index = codes.shape[0], k, codes.device, codes.device.index
+        self.n = _mx_packed(codes, scales, k)
+        self.k, self.device, self.index = k, codes.device, codes.device.index
         size = C.c_uint64()
         _check(lib().ts_mxfp4_matrix_bytes(self.n, k, C.byref(size)))
         self.data = torch.empty(size.value, dtype=torch.uint8, device=self.device)

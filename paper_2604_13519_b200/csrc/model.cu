@@ -448,7 +448,7 @@ ts_status run_mx(ts_model *m, int epi, const CUtensorMap &tw, uint64_t w, int N,
   g.y = out; g.ldy = N; g.y_type = ts::MX_F32; g.vec = 1;
   g.out = out; g.act_out = act_out; g.act_rows = L.rows_alloc; g.out_planes = m->planes; g.amax = amax;
   const ts::MxInput in{x, m->planes == 2 ? ts::MX_PAIR : ts::MX_BF16, M, K, K, (long long)L.rows_alloc * K};
-  const ts::MxPlan p = ts::mx_plan(M, g.tiles, g.n_kb, ts::mx_planes_of(in.type), m->n_sms);
+  const ts::MxPlan p = ts::mx_plan(M, g.tiles, g.n_kb, ts::mx_planes_of(in.type), m->n_sms, m->max_clusters);
   const bool pdl = m->use_pdl && !m->profiling;
   if (!p.own) {
     CU_TRY(ts::launch_mx_input(in, m->WS(L.mx), p, m->st, pdl));

@@ -12,11 +12,17 @@
 
 namespace ts {
 ts_status set_error(ts_status code, const char *fmt, ...);   // model.cu
-int gemm_max_clusters(int cluster, size_t smem_budget);
 
 namespace {
 
 constexpr int kConvThreads = 256, kConvUnroll = 4;   // groups of eight elements: a block's threads take four each
+
+// How the conversions walk a matrix.
+//   kFlat: rows follow one another and end with whole MX blocks: one long row.  kRows: rows can be read 16 bytes at a time.  In both a
+//   thread takes eight elements at a time, four neighbouring threads an MX block, and a block of threads four such rounds.
+//   kLanes: any alignment.  A lane takes one element, a warp an MX block, eight blocks at a time, so that accesses stay contiguous (with
+//   eight elements per thread a warp's stores of four bytes each went to 32 sectors: 2047 x 8190 fp32 72 us).
+enum : int { kFlat = 0, kRows = 1, kLanes = 2 };
 
 // Where group u of a block's groups of eight lies: row and first column.  (One 64-bit division per block, 32-bit ones per group.)
 struct Place { long long row; int col; };
@@ -46,6 +52,11 @@ __device__ __forceinline__ uint32_t to_e2m1x8(const float (&v)[8]) {
       : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
   return d;
 }
+__device__ __forceinline__ uint32_t to_e2m1x2(float lo, float hi) {
+  uint32_t d;
+  asm("{\n\t.reg .b8 a;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tmov.b32 %0, {a, a, a, a};\n\t}" : "=r"(d) : "f"(lo), "f"(hi));
+  return d & 255u;
+}
 // Two codes -> two fp32 values
 __device__ __forceinline__ float2 from_e2m1x2(uint32_t byte) {
   uint32_t h;
@@ -53,83 +64,179 @@ __device__ __forceinline__ float2 from_e2m1x2(uint32_t byte) {
   return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
 
-// Four neighbouring threads share an MX block.  The largest magnitude is found on the bits (a NaN is larger than an infinity, which
-// is larger than all numbers), its exponent field e gives the scale byte: floor(log2) - 2 + 127 = e - 2, at least 0 (numbers below
-// 2^-125 and zeros), 255 where the block has an infinity or NaN.
-template <int TYPE, bool VEC>
+// The largest magnitude of an MX block is found on the bits (a NaN is larger than an infinity, which is larger than all numbers); its
+// exponent field e gives the scale byte: floor(log2) - 2 + 127 = e - 2, at least 0 (numbers below 2^-125 and zeros), 255 where the
+// block has an infinity or NaN.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+  const uint32_t e = top >> 23;
+  return e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
+}
+// 2^(127 - s): exact, and no result that matters is subnormal
+__device__ __forceinline__ float scale_inverse(uint32_t s) { return s == 255u ? 0.f : __uint_as_float((254u - s) << 23); }
+// 2^(s - 127); 2^-127 is subnormal
+__device__ __forceinline__ float scale_value(uint32_t s) {
+  return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s << 23);
+}
+
+template <int TYPE, int MODE>
 __global__ void __launch_bounds__(kConvThreads)
-mx_quantise_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols, long long ldx, int nb, uint32_t *codes, uint8_t *scales) {
-  const Placer pl(4 * nb);
-  float v[kConvUnroll][8];
-  Place at[kConvUnroll];
+mx_quantise_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols, long long ldx, int nb, uint8_t *codes, uint8_t *scales,
+                   long long groups) {
+  if constexpr (MODE == kLanes) {
+    // groups: of eight MX blocks, per * rows of them
+    const uint32_t w = blockIdx.x * (kConvThreads / 32) + (threadIdx.x >> 5), per = (nb + 8) / 8, row = w / per;   // (fewer than 2^32 fit any memory)
+    const int lane = threadIdx.x & 31, b0 = (int)(w - row * per) * 8;
+    if (row >= rows) return;
+    const typename MxElem<TYPE>::raw *p = x + row * ldx;
+    uint8_t *row_codes = codes + ((long long)row * nb + b0) * 16, *row_scales = scales + (long long)row * nb + b0;
+    float v[8];
 #pragma unroll
-  for (int i = 0; i < kConvUnroll; ++i) {
-    at[i] = pl.at(i * kConvThreads + threadIdx.x);
-    if (at[i].row < rows) {
-      MxRaw8<TYPE> x8;
-      mx_fetch8<TYPE>(x + at[i].row * ldx, 0, true, at[i].col, cols, VEC, x8);
-      mx_widen8<TYPE>(x8, v[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    for (int i = 0; i < 8; ++i) {
+      const int c = (b0 + i) * kMxBlock + lane;
+      v[i] = c < cols ? mx_to_f32<TYPE>(p[c]) : 0.f;
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kConvUnroll; ++i) {
-    uint32_t top = 0;
+    for (int i = 0; i < 8; ++i) {
+      if (b0 + i >= nb) break;
+      const uint32_t s = scale_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v[i]) & 0x7fffffffu));
+      const float u = s == 255u ? 0.f : v[i] * scale_inverse(s);
+      const float next = __shfl_down_sync(0xffffffffu, u, 1);
+      if ((lane & 1) == 0) row_codes[i * 16 + (lane >> 1)] = (uint8_t)to_e2m1x2(u, next);
+      if (lane == 0) row_scales[i] = (uint8_t)s;
+    }
+  } else {
+    const long long g0 = (long long)blockIdx.x * (kConvThreads * kConvUnroll) + threadIdx.x;
+    MxRaw8<TYPE> raw[kConvUnroll];
+    long long at[kConvUnroll];   // the group's number in codes, -1: none
+    if constexpr (MODE == kFlat) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t e = top >> 23, s = e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
-    const float f = __uint_as_float((254u - min(s, 252u)) << 23);   // 2^(127 - s): exact, and no result that matters is subnormal
-    float u[8];
+      for (int i = 0; i < kConvUnroll; ++i) {
+        at[i] = g0 + i * kConvThreads < groups ? g0 + i * kConvThreads : -1;
+        mx_fetch8<TYPE>(x + (at[i] < 0 ? 0 : at[i]) * 8, 0, at[i] >= 0, 0, 8, true, raw[i]);
+      }
+    } else {
+      const Placer pl(4 * nb);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) u[j] = s == 255u ? 0.f : v[i][j] * f;
-    const uint32_t c = to_e2m1x8(u);
-    if (at[i].row < rows) {
-      const long long b = at[i].row * nb + (at[i].col >> 5);
-      codes[b * 4 + ((at[i].col >> 3) & 3)] = c;
-      if ((threadIdx.x & 3) == 0) scales[b] = (uint8_t)s;
+      for (int i = 0; i < kConvUnroll; ++i) {
+        const Place q = pl.at(i * kConvThreads + threadIdx.x);
+        at[i] = q.row < rows ? q.row * (4ll * nb) + (q.col >> 3) : -1;
+        mx_fetch8<TYPE>(x + (at[i] < 0 ? 0 : q.row) * ldx, 0, at[i] >= 0, q.col, cols, true, raw[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kConvUnroll; ++i) {
+      float v[8];
+      mx_widen8<TYPE>(raw[i], v);
+      uint32_t top = 0;
+      if constexpr (TYPE == MX_BF16) {   // (two at a time: their bits are the upper halves of fp32's)
+        const uint32_t *h = reinterpret_cast<const uint32_t *>(raw[i].r);
+        uint32_t m = __vmaxu2(__vmaxu2(h[0] & 0x7fff7fffu, h[1] & 0x7fff7fffu), __vmaxu2(h[2] & 0x7fff7fffu, h[3] & 0x7fff7fffu));
+        top = max(m & 0xffff0000u, m << 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const uint32_t s = scale_byte(top);
+      const float f = scale_inverse(s);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = s == 255u ? 0.f : v[j] * f;
+      const uint32_t c = to_e2m1x8(v);
+      if (at[i] >= 0) {
+        reinterpret_cast<uint32_t *>(codes)[at[i]] = c;
+        if ((threadIdx.x & 3) == 0) scales[at[i] >> 2] = (uint8_t)s;
+      }
     }
   }
 }
 
-template <int TYPE, bool VEC>
+template <int TYPE, int MODE>
 __global__ void __launch_bounds__(kConvThreads)
-mx_dequantise_kernel(const uint32_t *codes, const uint8_t *scales, long long rows, int cols, int nb, typename MxElem<TYPE>::raw *y, long long ldy) {
+mx_dequantise_kernel(const uint8_t *codes, const uint8_t *scales, long long rows, int cols, int nb, typename MxElem<TYPE>::raw *y, long long ldy,
+                     long long groups) {
   typedef typename MxElem<TYPE>::raw raw;
-  const Placer pl(4 * nb);
-  uint32_t c[kConvUnroll], s[kConvUnroll];
-  Place at[kConvUnroll];
+  if constexpr (MODE == kLanes) {
+    // A warp takes 256 elements as the other modes do, eight to a lane, and turns them in shared memory.  They begin at a multiple of 32
+    // elements in memory, wherever a row begins, so that the stores are whole lines.
+    __shared__ float turned[kConvThreads / 32][256 + 8];
+    const uint32_t w = blockIdx.x * (kConvThreads / 32) + (threadIdx.x >> 5), per = (nb + 8) / 8, row = w / per;
+    if (row >= rows) return;
+    const int lane = threadIdx.x & 31;
+    raw *d = y + row * ldy;
+    float *mine = turned[threadIdx.x >> 5];
+    // the warp's columns c0 .. c0 + 255 lie in the groups of eight from g0 on, `off` elements into them
+    const int c0 = (int)(w - row * per) * 256 - (int)((uintptr_t)d / sizeof(raw) % 32), g0 = c0 >> 3, off = c0 & 7;
+    const uint32_t *row_codes = reinterpret_cast<const uint32_t *>(codes) + (long long)row * nb * 4;
+    const uint8_t *row_scales = scales + (long long)row * nb;
+    for (int g = lane; g < 33; g += 32) {
+      const int at = max(0, min(g0 + g, 4 * nb - 1));
+      const uint32_t c = __ldg(row_codes + at);
+      const float f = scale_value(__ldg(row_scales + (at >> 2)));
 #pragma unroll
-  for (int i = 0; i < kConvUnroll; ++i) {
-    at[i] = pl.at(i * kConvThreads + threadIdx.x);
-    if (at[i].row >= rows) continue;
-    const long long b = at[i].row * nb + (at[i].col >> 5);
-    c[i] = __ldg(codes + b * 4 + ((at[i].col >> 3) & 3));
-    s[i] = __ldg(scales + b);
-  }
-#pragma unroll
-  for (int i = 0; i < kConvUnroll; ++i) {
-    if (at[i].row >= rows || at[i].col >= cols) continue;
-    // 2^(s - 127); 2^-127 is subnormal
-    const float f = s[i] == 255u ? __uint_as_float(0x7fc00000u) : s[i] == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s[i] << 23);
-    __align__(16) raw r[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 t = from_e2m1x2(c[i] >> (8 * j));
-      r[2 * j] = mx_from_f32<TYPE>(t.x * f);
-      r[2 * j + 1] = mx_from_f32<TYPE>(t.y * f);
+      for (int j = 0; j < 4; ++j) {
+        const float2 t = from_e2m1x2(c >> (8 * j));
+        mine[8 * g + 2 * j] = t.x * f;
+        mine[8 * g + 2 * j + 1] = t.y * f;
+      }
     }
-    raw *d = y + at[i].row * ldy + at[i].col;
-    if (VEC && at[i].col + 8 <= cols) {
+    __syncwarp();
 #pragma unroll
-      for (int j = 0; j < (int)sizeof(raw) / 2; ++j) reinterpret_cast<uint4 *>(d)[j] = reinterpret_cast<const uint4 *>(r)[j];
+    for (int i = 0; i < 8; ++i) {
+      const int col = c0 + 32 * i + lane;
+      if (col >= 0 && col < cols) d[col] = mx_from_f32<TYPE>(mine[off + 32 * i + lane]);
+    }
+  } else {
+    const long long g0 = (long long)blockIdx.x * (kConvThreads * kConvUnroll) + threadIdx.x;
+    uint32_t c[kConvUnroll], s[kConvUnroll];
+    long long at[kConvUnroll];
+    raw *d[kConvUnroll];
+    int left[kConvUnroll];   // elements of the row from the group's first on
+    if constexpr (MODE == kFlat) {
+#pragma unroll
+      for (int i = 0; i < kConvUnroll; ++i) {
+        at[i] = g0 + i * kConvThreads < groups ? g0 + i * kConvThreads : -1;
+        d[i] = y + at[i] * 8;
+        left[i] = 8;
+      }
     } else {
+      const Placer pl(4 * nb);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (at[i].col + j < cols) d[j] = r[j];
+      for (int i = 0; i < kConvUnroll; ++i) {
+        const Place q = pl.at(i * kConvThreads + threadIdx.x);
+        at[i] = q.row < rows && q.col < cols ? q.row * (4ll * nb) + (q.col >> 3) : -1;
+        d[i] = y + q.row * ldy + q.col;
+        left[i] = cols - q.col;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kConvUnroll; ++i) {
+      c[i] = at[i] < 0 ? 0 : __ldg(reinterpret_cast<const uint32_t *>(codes) + at[i]);
+      s[i] = at[i] < 0 ? 0 : __ldg(scales + (at[i] >> 2));
+    }
+#pragma unroll
+    for (int i = 0; i < kConvUnroll; ++i) {
+      if (at[i] < 0) continue;
+      const float f = scale_value(s[i]);
+      __align__(16) raw r[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 t = from_e2m1x2(c[i] >> (8 * j));
+        r[2 * j] = mx_from_f32<TYPE>(t.x * f);
+        r[2 * j + 1] = mx_from_f32<TYPE>(t.y * f);
+      }
+      if (left[i] >= 8) {
+        if (sizeof(raw) == 4 && ((uintptr_t)d[i] & 31) == 0) {
+          st_global_v8(reinterpret_cast<float *>(d[i]), reinterpret_cast<const uint32_t *>(r));   // (whole sectors)
+        } else {
+#pragma unroll
+          for (int j = 0; j < (int)sizeof(raw) / 2; ++j) reinterpret_cast<uint4 *>(d[i])[j] = reinterpret_cast<const uint4 *>(r)[j];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < left[i]) d[i][j] = r[j];
+      }
     }
   }
 }
@@ -187,13 +294,35 @@ unsigned conv_blocks(long long rows, int per_row) {
     case MX_F16: if (vec) F(MX_F16, true); else F(MX_F16, false); break;         \
     default: if (vec) F(MX_F32, true); else F(MX_F32, false); break;             \
   }
+#define MX_BY_MODE(type, mode, F)                                                                                               \
+  switch (type) {                                                                                                               \
+    case MX_BF16: if (mode == kFlat) F(MX_BF16, kFlat); else if (mode == kRows) F(MX_BF16, kRows); else F(MX_BF16, kLanes); break;  \
+    case MX_F16: if (mode == kFlat) F(MX_F16, kFlat); else if (mode == kRows) F(MX_F16, kRows); else F(MX_F16, kLanes); break;      \
+    default: if (mode == kFlat) F(MX_F32, kFlat); else if (mode == kRows) F(MX_F32, kRows); else F(MX_F32, kLanes); break;          \
+  }
+
+// How a matrix is walked, and the blocks of threads that takes.
+static int conv_mode(const void *p, int type, int rows, int cols, long long ld, unsigned *blocks, long long *groups) {
+  const int nb = (cols + kMxBlock - 1) / kMxBlock;
+  *groups = (long long)rows * 4 * nb;
+  const int mode = !mx_aligned(p, ld, type) ? kLanes : cols % kMxBlock == 0 && (ld == cols || rows == 1) ? kFlat : kRows;
+  if (mode == kLanes) {
+    const long long warps = (long long)rows * ((nb + 8) / 8);   // (a row to be read takes one in eight MX blocks, one to be written may take one more)
+    *blocks = (unsigned)((warps + kConvThreads / 32 - 1) / (kConvThreads / 32));
+  } else {
+    *blocks = conv_blocks(rows, 4 * nb);
+  }
+  return mode;
+}
 
 cudaError_t launch_mx_quantise(const void *x, int type, int rows, int cols, long long ldx, uint8_t *codes, uint8_t *scales, cudaStream_t st) {
   const int nb = (cols + kMxBlock - 1) / kMxBlock;
   if (rows <= 0 || cols <= 0) return cudaSuccess;
-  const bool vec = mx_aligned(x, ldx, type);
-#define F(T, V) mx_quantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const MxElem<T>::raw *)x, rows, cols, ldx, nb, (uint32_t *)codes, scales)
-  MX_BY_TYPE(type, vec, F)
+  unsigned blocks;
+  long long groups;
+  const int mode = conv_mode(x, type, rows, cols, ldx, &blocks, &groups);
+#define F(T, V) mx_quantise_kernel<T, V><<<blocks, kConvThreads, 0, st>>>((const MxElem<T>::raw *)x, rows, cols, ldx, nb, codes, scales, groups)
+  MX_BY_MODE(type, mode, F)
 #undef F
   return cudaGetLastError();
 }
@@ -202,9 +331,11 @@ cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, in
                                  cudaStream_t st) {
   const int nb = (cols + kMxBlock - 1) / kMxBlock;
   if (rows <= 0 || cols <= 0) return cudaSuccess;
-  const bool vec = mx_aligned(y, ldy, type);
-#define F(T, V) mx_dequantise_kernel<T, V><<<conv_blocks(rows, 4 * nb), kConvThreads, 0, st>>>((const uint32_t *)codes, scales, rows, cols, nb, (MxElem<T>::raw *)y, ldy)
-  MX_BY_TYPE(type, vec, F)
+  unsigned blocks;
+  long long groups;
+  const int mode = conv_mode(y, type, rows, cols, ldy, &blocks, &groups);
+#define F(T, V) mx_dequantise_kernel<T, V><<<blocks, kConvThreads, 0, st>>>(codes, scales, rows, cols, nb, (MxElem<T>::raw *)y, ldy, groups)
+  MX_BY_MODE(type, mode, F)
 #undef F
   return cudaGetLastError();
 }
@@ -238,7 +369,7 @@ cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, c
   const MxScratch w = mx_scratch((in.cols + kMxTileK - 1) / kMxTileK, mx_planes_of(in.type), p);
   uint8_t *out = (uint8_t *)scratch;
   int *flags = (int *)(out + w.flags);
-  const int n_flags = p.stream ? p.chunks * p.ctas : 0;
+  const int n_flags = p.stream ? (p.apart ? p.chunks : 1) * p.ctas : 0;
   const bool vec = mx_aligned(in.x, in.ldx, in.type) && (in.type != MX_PAIR || in.pair % 8 == 0);
   if (in.type == MX_PAIR) return vec ? planes8<MX_PAIR, true>(in, out, p.Mc, flags, n_flags, st, pdl) : planes8<MX_PAIR, false>(in, out, p.Mc, flags, n_flags, st, pdl);
 #define F(T, V) return planes8<T, V>(in, out, p.Mc, flags, n_flags, st, pdl)
@@ -271,6 +402,7 @@ using ts::EncodeTiledFn;
 // What a device offers, asked for once per device.
 struct MxDevice {
   int sms = 0;
+  int fits[9] = {};   // (see mx_plan)
 };
 constexpr int kMaxDevices = 64;
 MxDevice g_dev[kMaxDevices];
@@ -296,6 +428,7 @@ ts_status device_of_call(MxDevice *out) {
       g_encode.store((EncodeTiledFn)fn, std::memory_order_release);
     }
     g_dev[dev].sms = sms;   // (two threads that come here at once store the same)
+    ts::mx_fits(g_dev[dev].fits);
     g_dev_known.fetch_or(1ull << dev, std::memory_order_release);
   }
   *out = g_dev[dev];
@@ -439,7 +572,7 @@ ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
   g.vec = a->ldy % 4 == 0 && (uintptr_t)a->y % (4 * ysz) == 0;
   const ts::MxInput in{a->x, a->x_type, (int)M, (int)K, a->ldx, 0};
   const int planes = ts::mx_planes_of(a->x_type);
-  const ts::MxPlan p = ts::mx_plan((int)M, g.tiles, g.n_kb, planes, d.sms);
+  const ts::MxPlan p = ts::mx_plan((int)M, g.tiles, g.n_kb, planes, d.sms, d.fits);
   const uint64_t need = ts::mx_scratch(g.n_kb, planes, p).bytes;
   if (need && (!a->workspace || a->workspace_bytes < need || (uintptr_t)a->workspace % 128))
     return set_error(TS_ERR_ARG, "workspace of %llu bytes, 128-byte aligned, needed for these rows", (unsigned long long)need);

@@ -74,6 +74,10 @@ __device__ __forceinline__ void mx_fetch8(const typename MxElem<TYPE>::raw *p, l
   for (int h = 0; h < kArrays; ++h) {
     const typename MxElem<TYPE>::raw *q = p + h * pair;
     if (vec && there && c + 8 <= cols) {
+      if (sizeof(x.r[0]) == 4 && ((uintptr_t)(q + c) & 31) == 0) {
+        ld_global_v8(q + c, reinterpret_cast<uint32_t *>(x.r));   // (whole sectors)
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < (int)sizeof(x.r[0]) / 2; ++i) reinterpret_cast<uint4 *>(x.r + 8 * h)[i] = __ldg(reinterpret_cast<const uint4 *>(q + c) + i);
     } else {
@@ -184,10 +188,12 @@ template <int EPI> __device__ __forceinline__ void mx_finish(const MxArgs &g, lo
 }
 #endif
 
-// How a product is dealt out: activation rows per chunk (a multiple of 8, planes x rows one of 16), chunks, and whether each of them is
-// a launch of its own; runs of k-blocks (stream) or a tile to each of `ctas` clusters; whether it makes the planes itself.
-struct MxPlan { int Mc, chunks, ctas, cluster; bool apart, stream, own; };
-MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms);
+// How a product is dealt out: activation rows per chunk (a multiple of 8, planes x rows one of 16), chunks; runs of k-blocks
+// (stream; apart: a launch per chunk) or a tile to each of `ctas` clusters; whether it makes the planes itself.
+struct MxPlan { int Mc, chunks, ctas, cluster; bool stream, apart, own; };
+// fits[c]: clusters of c CTAs that the device runs at once (mx_fits); null: none are made.
+MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits);
+void mx_fits(int (&fits)[9]);
 
 // Activations, and the scratch memory of a product with them: planes, and for products dealt out in runs flags and slabs.
 struct MxInput {

@@ -128,17 +128,20 @@ __device__ __forceinline__ void prod_block(uint32_t sa, uint32_t sf, uint32_t d,
 
 // eight rows' sums of this thread's feature, planes added
 __device__ __forceinline__ void prod_sums(const MxArgs &g, uint32_t taddr, float (&v)[8]) {
-  uint32_t r[8];
-  tmem_ld8(taddr, r);
+  constexpr int kMostPlanes = 5;
+  uint32_t r[kMostPlanes][8];
+#pragma unroll
+  for (int p = 0; p < kMostPlanes; ++p)
+    if (p < g.planes) tmem_ld8(taddr + p * g.Mc, r[p]);
   tmem_wait_ld();
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
-  for (int p = 1; p < g.planes; ++p) {
-    tmem_ld8(taddr + p * g.Mc, r);
-    tmem_wait_ld();
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[0][i]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(r[i]);
-  }
+  for (int p = 1; p < kMostPlanes; ++p)
+    if (p < g.planes) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(r[p][i]);
+    }
 }
 
 template <int EPI, bool kStream, bool kOwn, int TYPE>
@@ -301,15 +304,17 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
     }
   } else if (kStream) {
     // ------------------------------------------------------------------ epilogue of a run
-    // Thread <-> feature out of tensor memory; through shared memory, eight rows at a time, to a warp per row with four features per
-    // lane, so that what goes out is whole lines.
+    // Thread <-> feature out of tensor memory, where partial sums go to and come from a slab as they are (a warp's 32 features are a line);
+    // finished ones through shared memory, eight rows at a time, to a warp per row with four features per lane.
     const int q = warp & 3;                       // TMEM lane quarter this warp may read
+    const int f = q * 32 + lane;                  // this thread's feature of a tile
     const uint32_t stg = smem_u32(staging);
     pdl_wait();   // (flags are cleared by the kernel before; outputs may still be read by its consumers)
     int j = 0, turn = 0;
     bool alive = true;   // (all warps go through the same barriers whatever becomes of a wait; after one has expired none is waited for)
     for (long long hi = u1; hi > u0; ++j) {
       const ProdSeg t = prod_seg(g, u0, hi);
+      hi -= t.kb1 - t.kb0;
       const int b = n_acc == 2 ? j & 1 : 0, use = n_acc == 2 ? j >> 1 : j;
       bool ok = alive && __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_full[b]), use & 1));
       if (!ok && lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
@@ -317,54 +322,65 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
       tc_fence_after();
       ok = ok && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
       const int tile = t.item / g.chunks, z = t.item - tile * g.chunks, m0 = z * g.Mc, M = min(g.Mc, g.M - m0);
-      const bool whole = t.kb1 == g.n_kb;         // this CTA finishes the tile
-      int before = cta;                           // CTAs [before, cta) have its earlier k-blocks
-      if (whole && t.kb0 > 0) {
+      const uint32_t taddr = tmem_base + b * acc_cols + ((uint32_t)(q * 32) << 16);
+      auto emptied = [&]() {   // the sums are out of tensor memory
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[b]));
+      };
+      if (t.kb1 != g.n_kb) {   // another CTA finishes the tile
+        float *slab = g.slabs + (size_t)cta * g.Mc * kMxTileN + f;
+        for (int c0 = 0; c0 < M; c0 += 8) {
+          float v[8];
+          prod_sums(g, taddr + c0, v);
+          if (c0 + 8 >= M) emptied();
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (ok) __stcg(slab + (c0 + i) * kMxTileN, v[i]);   // (rows behind the last one too: Mc is a multiple of eight)
+        }
+        __threadfence();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (warp == 2 && lane == 0 && ok) asm volatile("st.release.gpu.global.b32 [%0], %1;" ::"l"(g.flags + cta), "r"(1) : "memory");
+        continue;
+      }
+      int before = cta;   // CTAs [before, cta) have its earlier k-blocks
+      if (t.kb0 > 0) {
         const long long first = (long long)t.item * g.n_kb;
         do --before;
         while (prod_start(g, before, G) > first);
         for (int c = before; ok && c < cta; ++c) ok = __all_sync(0xffffffffu, wait_flag(g.flags + c));
         if (!ok && lane == 0) prod_error(g, DEV_TIMEOUT_GRID);
       }
-      const uint32_t taddr = tmem_base + b * acc_cols + ((uint32_t)(q * 32) << 16);
+      float part[8];   // the CTAs' partial sums, eight rows ahead of use
+      auto fetch = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[i] = 0.f;
+        for (int c = before; ok && c0 < M && c < cta; ++c) {
+          const float *slab = g.slabs + ((size_t)c * g.Mc + c0) * kMxTileN + f;
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = __ldcg(slab + i * kMxTileN);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) part[i] += x[i];
+        }
+      };
+      fetch(0);
       const int n = tile * kMxTileN + lane * 4;
       for (int c0 = 0; c0 < M; c0 += 8, turn ^= 1) {
         const uint32_t buf = stg + turn * (kProdStaging / 2);
         float v[8];
         prod_sums(g, taddr + c0, v);
-        if (c0 + 8 >= M) {   // (the sums are out of tensor memory)
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[b]));
-        }
+        if (c0 + 8 >= M) emptied();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) st_shared_f32(buf + (i * kMxTileN + q * 32 + lane) * 4, v[i]);
+        for (int i = 0; i < 8; ++i) st_shared_f32(buf + (i * kMxTileN + f) * 4, v[i] + part[i]);
+        fetch(c0 + 8);
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        for (int i = warp - 2; i < 8 && c0 + i < M; i += 4) {
+        for (int i = warp - 2; ok && i < 8 && c0 + i < M; i += 4) {
           const uint4 u = ld_shared_v4(buf + (i * kMxTileN + lane * 4) * 4);
-          if (!ok) continue;
-          if (!whole) {
-            __stcg(reinterpret_cast<uint4 *>(g.slabs + ((size_t)cta * g.Mc + c0 + i) * kMxTileN) + lane, u);
-            continue;
-          }
-          float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
-          if (before < cta) {
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int c = before; c < cta; ++c) {
-              const float4 p = __ldcg(reinterpret_cast<const float4 *>(g.slabs + ((size_t)c * g.Mc + c0 + i) * kMxTileN) + lane);
-              sum.x += p.x; sum.y += p.y; sum.z += p.z; sum.w += p.w;
-            }
-            w[0] += sum.x; w[1] += sum.y; w[2] += sum.z; w[3] += sum.w;
-          }
+          const float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
           mx_finish<EPI>(g, g.row0 + m0 + c0 + i, n, w, lane);
         }
       }
-      if (!whole) {
-        __threadfence();
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (warp == 2 && lane == 0 && ok) asm volatile("st.release.gpu.global.b32 [%0], %1;" ::"l"(g.flags + cta), "r"(1) : "memory");
-      }
-      hi -= t.kb1 - t.kb0;
     }
   } else if (warp < 6) {
     // ------------------------------------------------------------------ epilogue of a tile
@@ -472,22 +488,35 @@ static size_t prod_stage_bytes(int planes, int Mc) {
   return kProdW + ((512 + mx_x_block(ncols) + 1023) & ~1023);
 }
 
-// Rows per chunk: all of them up to 224 instruction columns, else equal chunks of fewer.  Then CTAs, two to an SM: runs of k-blocks where
-// there are more tiles than places, else clusters of as many as there is room for, eight at most.  Up to 64 rows neither the cut along K nor
-// the order of the sums may depend on the number of rows: chunks are then launches of their own.
+// Rows per chunk: all of them up to 224 instruction columns, else equal chunks of fewer.  Then CTAs, two to an SM: clusters of as many
+// along K as there is room for, eight at most, or runs of k-blocks.  Up to 64 rows (fp32: 32, which is a chunk) neither the cut along K nor
+// the order of the sums may depend on the number of rows: chunks do not count then, and where runs are dealt out each is a launch of its
+// own.
+//
+// Runs where there are more tiles than places, and where tiles do not come out even over the SMs and the time that costs is worth the
+// second exchange at a run's end, 7 to 12 us.  An SM takes a block in about 256 + 2 x columns cycles, the time of its bytes through shared
+// memory (weights 16 KB, columns x 128, all of it written and read, 128 a cycle).  301 rows of fp16 x 4096 x 12288, 160 tiles: 66 -> 63 us;
+// 64 rows x 24576 x 4096, 192 tiles: 21 us and 28 in runs, 112 rows 31 and 39.
 constexpr int kOwnRows = 2;     // most rows whose planes the product makes itself
-constexpr int kSameRows = 64;
-MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms) {
+constexpr int kRunCycles = 25000;
+MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits) {
   MxPlan p{};
   const int step = planes % 2 ? 16 : 8, most = kProdAcc / planes / step * step;   // (the instruction's N, planes x rows, is a multiple of 16)
   p.chunks = (M + most - 1) / most;
   p.Mc = ((M + p.chunks - 1) / p.chunks + step - 1) / step * step;
   p.chunks = (M + p.Mc - 1) / p.Mc;
-  p.apart = M <= kSameRows;
-  const long long items = (long long)tiles * (p.apart ? 1 : p.chunks), places = (long long)kProdCtas * std::min(n_sms, kMxMostSms);
-  p.stream = items > places && (p.apart || p.chunks == 1);
-  p.cluster = p.stream ? 1 : (int)std::max<long long>(1, std::min<long long>(std::min(8, n_kb), places / items));
-  p.ctas = (int)(p.stream ? places : items);
+  n_sms = std::min(n_sms, kMxMostSms);
+  const bool same = M <= (planes == 5 ? 32 : 64);
+  const long long items = (long long)tiles * (same ? 1 : p.chunks), places = (long long)kProdCtas * n_sms;
+  const long long uneven = ((items + n_sms - 1) / n_sms * n_sms - items) * n_kb * (256 + 2 * (same ? 32 : planes * p.Mc)) / n_sms;
+  p.apart = same && p.chunks > 1;
+  p.stream = items > n_sms && items * n_kb >= 4 * places && ((items > places && (same || p.chunks == 1)) || uneven > kRunCycles);
+  // (A tenth more than are needed must fit: how many do depends on how the device's SMs are grouped, and one that finds its place taken runs
+  // as a second wave.  6144 x 4096 at 32 rows: 48 clusters of six, of which 45 fit, 15.2 us; of five 9.6.)
+  p.cluster = 1;
+  for (int c = 2; fits && !p.stream && c <= 8 && c <= n_kb; ++c)
+    if (fits[c] * 10ll >= items * 11) p.cluster = c;
+  p.ctas = (int)(p.stream ? places : (long long)tiles * p.chunks);
   p.own = !p.stream && M <= kOwnRows;
   return p;
 }
@@ -495,7 +524,7 @@ MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms) {
 MxScratch mx_scratch(int n_kb, int planes, const MxPlan &p) {
   MxScratch w{};
   if (p.own) return w;
-  const uint64_t n_flags = p.stream ? (uint64_t)p.chunks * p.ctas : 0;   // (a launch's flags are its own, the slabs are reused)
+  const uint64_t n_flags = p.stream ? (uint64_t)(p.apart ? p.chunks : 1) * p.ctas : 0;   // (a launch's flags are its own, the slabs are reused)
   w.flags = (uint64_t)p.chunks * n_kb * mx_x_block(planes * p.Mc);
   w.slabs = w.flags + (n_flags * 4 + 127) / 128 * 128;
   w.bytes = w.slabs + (p.stream ? (uint64_t)p.ctas * p.Mc * kMxTileN * 4 : 0);
@@ -503,12 +532,18 @@ MxScratch mx_scratch(int n_kb, int planes, const MxPlan &p) {
 }
 uint64_t mx_scratch_most(int rows, int n_kb, int planes) {
   if (!rows || !n_kb) return 0;
-  MxPlan p = mx_plan(rows, 1, n_kb, planes, 1);
-  if (p.chunks > 1) p.Mc = mx_plan(1 << 20, 1, 1, planes, 1).Mc;   // (equal chunks may be larger for fewer rows)
+  MxPlan p = mx_plan(rows, 1, n_kb, planes, 1, nullptr);
+  if (p.chunks > 1) p.Mc = mx_plan(1 << 20, 1, 1, planes, 1, nullptr).Mc;   // (equal chunks may be larger for fewer rows)
   p.own = false;
-  p.stream = true;
+  p.stream = p.apart = true;
   p.ctas = kProdCtas * kMxMostSms;
   return mx_scratch(n_kb, planes, p).bytes;
+}
+
+int gemm_max_clusters(int cluster, size_t smem_budget);   // gemm_tcgen05.cu
+void mx_fits(int (&fits)[9]) {
+  fits[0] = 0;
+  for (int c = 1; c <= 8; ++c) fits[c] = gemm_max_clusters(c, 113 * 1024);
 }
 
 template <int EPI, bool kStream, bool kOwn, int TYPE>
@@ -570,8 +605,9 @@ cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const Mx
   const int acc = (ncols + 31) & ~31, sets = g.stages * (4 + 4 * ((ncols + 127) / 128));   // columns of an accumulator, of all scales
   g.n_acc = p.stream && 2 * acc + sets <= 256 ? 2 : 1;
   const size_t smem = g.stages * stage + fixed;
-  const int passes = p.apart ? p.chunks : 1;
-  g.chunks = p.apart ? 1 : p.chunks;
+  const bool apart = p.stream && p.apart;
+  const int passes = apart ? p.chunks : 1;
+  g.chunks = apart ? 1 : p.chunks;
   g.units = (long long)g.tiles * g.chunks * g.n_kb;
   if (g.stages < 2 || g.Mc % 8 || ncols % 16 || ncols > kProdAcc || g.n_acc * acc + sets > 256 || p.ctas < 1 || p.cluster < 1 || p.cluster > 8 ||
       p.cluster > g.n_kb || (p.stream && p.ctas > g.units) || (size_t)g.stages * stage < (size_t)g.Mc * kMxTileN * 4 || (p.own && passes != 1))
