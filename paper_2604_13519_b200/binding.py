@@ -687,15 +687,25 @@ def _on_device_of(index, stream, call, *args):
         _check(call(*args, stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)))
 
 
+def _mx_empty(shape, dtype, device, stream):
+    """Memory of the stream that it is written on (the caching allocator hands it out again in that stream's order)."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def ts_mxfp4_quantise(x, stream=None):
     """x: CUDA tensor [rows][cols], bf16, fp16 or fp32, rows contiguous.  Returns (codes uint8 [rows][16 nb], scales uint8
-    [rows][nb]), nb = ceil(cols / 32)."""
+    [rows][nb]), nb = ceil(cols / 32).  (This call and the next ones run on `stream`, or on the current stream of the tensor's
+    device, and what they return is that stream's memory.)"""
     import torch
     rows, cols, ldx = _mx_rows(x, "x")
     nb = (cols + 31) // 32
     device = x.device
-    codes = torch.empty((rows, 16 * nb), dtype=torch.uint8, device=device)
-    scales = torch.empty((rows, nb), dtype=torch.uint8, device=device)
+    codes = _mx_empty((rows, 16 * nb), torch.uint8, device, stream)
+    scales = _mx_empty((rows, nb), torch.uint8, device, stream)
     _on_device_of(device.index, stream, lib().ts_mxfp4_quantise, x.data_ptr(), _mx_type(x.dtype), rows, cols, ldx, codes.data_ptr(),
                   scales.data_ptr())
     return codes, scales
@@ -703,10 +713,9 @@ def ts_mxfp4_quantise(x, stream=None):
 
 def ts_mxfp4_dequantise(codes, scales, cols: int, dtype, out=None, stream=None):
     """The values of an MXFP4 matrix of `cols` columns, in `dtype` (bf16, fp16, fp32); written into `out` if it is given."""
-    import torch
     rows = _mx_packed(codes, scales, cols)
     if out is None:
-        out, ldy = torch.empty((rows, cols), dtype=dtype, device=codes.device), cols
+        out, ldy = _mx_empty((rows, cols), dtype, codes.device, stream), cols
     else:
         have, width, ldy = _mx_rows(out, "out")
         if out.dtype != dtype or (have, width) != (rows, cols) or out.device != codes.device:
@@ -725,20 +734,21 @@ class Mxfp4Matrix:
         self.k, self.device, self.index = k, codes.device, codes.device.index
         size = C.c_uint64()
         _check(lib().ts_mxfp4_matrix_bytes(self.n, k, C.byref(size)))
-        self.data = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        self.data = _mx_empty(size.value, torch.uint8, self.device, stream)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()     # (products may run on any stream)
         self.handle = ts_mxfp4_matrix()
         with torch.cuda.device(self.index):
             _check(lib().ts_mxfp4_matrix_init(C.byref(self.handle), self.data.data_ptr(), self.n, k))
         self._status_ptr, self._handle_ref = self.status.data_ptr(), C.pointer(self.handle)
         _on_device_of(self.index, stream, lib().ts_mxfp4_lay_out, codes.data_ptr(), scales.data_ptr(), self.n, k, self.data.data_ptr())
 
-    def workspace(self, rows: int, dtype):
+    def workspace(self, rows: int, dtype, stream=None):
         """Scratch memory for products of up to `rows` rows of `dtype`, which a caller may keep; one per stream."""
         import torch
         size = C.c_uint64()
         _check(lib().ts_mxfp4_product_workspace(rows, self.n, self.k, _mx_type(dtype), C.byref(size)))
-        return torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        return _mx_empty(size.value, torch.uint8, self.device, stream)
 
     def check(self):
         """Waits for the device and raises if a wait inside a product's kernel has expired since the last check."""
@@ -751,20 +761,19 @@ class Mxfp4Matrix:
 def ts_mxfp4_product(matrix: Mxfp4Matrix, x, dtype=None, out=None, workspace=None, stream=None):
     """y = x W^T: x CUDA tensor [rows][k], bf16, fp16 or fp32, rows contiguous; y [rows][n] in `dtype` (default: x's), written into `out`
     if it is given.  workspace: matrix.workspace(rows, x.dtype) or more; made here if it is not given."""
-    import torch
     rows, cols, ldx = _mx_rows(x, "x")
     if cols != matrix.k or x.device != matrix.device:
         raise ValueError(f"x must have {matrix.k} columns and lie on the matrix's device")
     n = matrix.n
     if out is None:
-        out = torch.empty((rows, n), dtype=dtype or x.dtype, device=matrix.device)
+        out = _mx_empty((rows, n), dtype or x.dtype, matrix.device, stream)
         ldy = n
     else:
         have, width, ldy = _mx_rows(out, "out")
         if (have, width) != (rows, n) or out.device != matrix.device or (dtype is not None and out.dtype != dtype):
             raise ValueError("out does not match the product")
     if workspace is None:
-        workspace = matrix.workspace(rows, x.dtype)
+        workspace = matrix.workspace(rows, x.dtype, stream)
     elif workspace.device != matrix.device:
         raise ValueError("the workspace must lie on the matrix's device")
     a = ts_mxfp4_product_args(matrix._handle_ref, rows, ldx, ldy, _mx_type(x.dtype), _mx_type(out.dtype), x.data_ptr(), out.data_ptr(),

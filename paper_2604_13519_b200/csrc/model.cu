@@ -445,13 +445,14 @@ ts_status run_mx(ts_model *m, int epi, const CUtensorMap &tw, uint64_t w, int N,
   ts::MxArgs g{};
   g.w = m->W(w); g.N = N; g.tiles = N / ts::kMxTileN; g.n_kb = (K + ts::kMxTileK - 1) / ts::kMxTileK;
   g.err = m->d_out() + L.o_err;
+  g.early = 1;
   g.y = out; g.ldy = N; g.y_type = ts::MX_F32; g.vec = 1;
   g.out = out; g.act_out = act_out; g.act_rows = L.rows_alloc; g.out_planes = m->planes; g.amax = amax;
   const ts::MxInput in{x, m->planes == 2 ? ts::MX_PAIR : ts::MX_BF16, M, K, K, (long long)L.rows_alloc * K};
   const ts::MxPlan p = ts::mx_plan(M, g.tiles, g.n_kb, ts::mx_planes_of(in.type), m->n_sms, m->max_clusters);
   const bool pdl = m->use_pdl && !m->profiling;
   if (!p.own) {
-    CU_TRY(ts::launch_mx_input(in, m->WS(L.mx), p, m->st, pdl));
+    CU_TRY(ts::launch_mx_input(in, m->WS(L.mx), p, true, m->st, pdl));
     m->launched(0);
   }
   g.stamp = m->stamp_slot();
@@ -1366,7 +1367,8 @@ ts_status ts_load_tensor(ts_model *m, int32_t kind, int32_t layer, const void *h
   if (c.weights == TS_WEIGHTS_MXFP4) {
     // quantised on the device, a chunk of rows at a time: codes, scales and, from the host, the rows themselves in the staging area
     const int64_t nb = (ec + ts::kMxBlock - 1) / ts::kMxBlock;
-    const int64_t per = std::max<int64_t>(1, (int64_t)((stage_bytes - 64) / (17 * (size_t)nb + (dev_src ? 0 : row_bytes))));
+    const int64_t per = (int64_t)((stage_bytes - 64) / (17 * (size_t)nb + (dev_src ? 0 : row_bytes)));
+    if (per < 1) return fail(TS_ERR_ARG, "a row of %lld elements does not fit the staging area (max_rows x vocab)", (long long)ec);
     uint8_t *stage = m->WS(L.logits);
     for (int64_t r0 = 0; r0 < er; r0 += per) {
       const int64_t nr = std::min(per, er - r0);
@@ -1408,7 +1410,8 @@ ts_status ts_load_tensor_mxfp4(ts_model *m, int32_t kind, int32_t layer, const v
   if (t.esz == 4 || kind == TS_W_EMBED) return fail(TS_ERR_ARG, "tensor kind %d is not a projection matrix: ts_load_tensor takes it", kind);
   const int64_t nb = (t.ec + ts::kMxBlock - 1) / ts::kMxBlock;
   const size_t stage_bytes = (size_t)m->L.step_rows_alloc * (size_t)m->c.vocab * 4;
-  const int64_t per = std::max<int64_t>(1, (int64_t)(stage_bytes / (17 * (size_t)nb)));
+  const int64_t per = (int64_t)(stage_bytes / (17 * (size_t)nb));
+  if (per < 1) return fail(TS_ERR_ARG, "a row of %lld elements does not fit the staging area (max_rows x vocab)", (long long)t.ec);
   uint8_t *stage = m->WS(m->L.logits);
   for (int64_t r0 = 0; r0 < t.er; r0 += per) {   // (through the staging area wherever they come from: no alignment is asked of them)
     const int64_t nr = std::min(per, t.er - r0);

@@ -265,9 +265,11 @@ mx_lay_out_kernel(const uint4 *codes, const uint8_t *scales, int n_rows, int n_f
 template <int TYPE, bool VEC>
 __global__ void __launch_bounds__(kConvThreads)
 mx_planes8_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols, long long ldx, long long pair, uint8_t *out, int ldo, int Mc,
-                  int planes, int *flags, int n_flags) {
-  pdl_launch_dependents();   // (the product waits for this kernel's end before it reads activations)
-  pdl_wait();                // (x may come from the kernel before, whose activations may be in the same scratch memory)
+                  int planes, int *flags, int n_flags, bool early) {
+  // (the product waits for this kernel's end before it reads activations, but fetches weights at once)
+  if (early) pdl_launch_dependents();
+  pdl_wait();   // (x may come from the kernel before, whose activations may be in the same scratch memory)
+  if (!early) pdl_launch_dependents();
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < n_flags; i += kConvThreads) flags[i] = 0;
   const long long i = (long long)blockIdx.x * kConvThreads + threadIdx.x;
@@ -351,7 +353,7 @@ cudaError_t launch_mx_lay_out(const uint8_t *codes, const uint8_t *scales, int n
 }
 
 template <int TYPE, bool VEC>
-static cudaError_t planes8(const MxInput &in, uint8_t *out, int Mc, int *flags, int n_flags, cudaStream_t st, bool pdl) {
+static cudaError_t planes8(const MxInput &in, uint8_t *out, int Mc, int *flags, int n_flags, bool early, cudaStream_t st, bool pdl) {
   const int ldo = (in.cols + kMxTileK - 1) / kMxTileK * kMxTileK;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(((long long)in.rows * (ldo / 8) + kConvThreads - 1) / kConvThreads));
@@ -363,16 +365,16 @@ static cudaError_t planes8(const MxInput &in, uint8_t *out, int Mc, int *flags, 
   cfg.attrs = at;
   cfg.numAttrs = pdl ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, mx_planes8_kernel<TYPE, VEC>, (const typename MxElem<TYPE>::raw *)in.x, (long long)in.rows, in.cols, in.ldx, in.pair,
-                            out, ldo, Mc, mx_planes_of(TYPE), flags, n_flags);
+                            out, ldo, Mc, mx_planes_of(TYPE), flags, n_flags, early);
 }
-cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st, bool pdl) {
+cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, bool early, cudaStream_t st, bool pdl) {
   const MxScratch w = mx_scratch((in.cols + kMxTileK - 1) / kMxTileK, mx_planes_of(in.type), p);
   uint8_t *out = (uint8_t *)scratch;
   int *flags = (int *)(out + w.flags);
   const int n_flags = p.stream ? (p.apart ? p.chunks : 1) * p.ctas : 0;
   const bool vec = mx_aligned(in.x, in.ldx, in.type) && (in.type != MX_PAIR || in.pair % 8 == 0);
-  if (in.type == MX_PAIR) return vec ? planes8<MX_PAIR, true>(in, out, p.Mc, flags, n_flags, st, pdl) : planes8<MX_PAIR, false>(in, out, p.Mc, flags, n_flags, st, pdl);
-#define F(T, V) return planes8<T, V>(in, out, p.Mc, flags, n_flags, st, pdl)
+  if (in.type == MX_PAIR) return vec ? planes8<MX_PAIR, true>(in, out, p.Mc, flags, n_flags, early, st, pdl) : planes8<MX_PAIR, false>(in, out, p.Mc, flags, n_flags, early, st, pdl);
+#define F(T, V) return planes8<T, V>(in, out, p.Mc, flags, n_flags, early, st, pdl)
   MX_BY_TYPE(in.type, vec, F)
 #undef F
 }
@@ -576,7 +578,9 @@ ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
   const uint64_t need = ts::mx_scratch(g.n_kb, planes, p).bytes;
   if (need && (!a->workspace || a->workspace_bytes < need || (uintptr_t)a->workspace % 128))
     return set_error(TS_ERR_ARG, "workspace of %llu bytes, 128-byte aligned, needed for these rows", (unsigned long long)need);
-  if (!p.own) MX_TRY(ts::launch_mx_input(in, a->workspace, p, st, true));
+  // (the matrix may have been laid out by the kernel just before: nothing of it is read until that is done)
+  g.early = !p.own;
+  if (!p.own) MX_TRY(ts::launch_mx_input(in, a->workspace, p, false, st, true));
   CUtensorMap tw;
   std::memcpy(&tw, w->map, sizeof tw);
   MX_TRY(ts::launch_mx_product(ts::MX_STORE, tw, g, in, a->workspace, p, st, true, nullptr));

@@ -31,6 +31,7 @@ struct MxArgs {
   int N, M, row0;            // features, activation rows of this launch, the first one's place among all rows of the result
   int tiles, n_kb;           // 128-row tiles and 128-column blocks of the matrix
   int planes;                // planes of e4m3 numbers that are added
+  int early;                 // the matrix was written long ago: its blocks may be fetched before the previous kernel is done
   int Mc, chunks, stages, n_acc;   // filled in by the launcher: activation rows per tile of the result, their chunks, stages of the ring, accumulators
   long long units;           // tiles x chunks x k-blocks
   int *err;                  // device status word (null: not wanted)
@@ -213,7 +214,8 @@ inline bool mx_aligned(const void *p, long long ld, int type) { return ((uintptr
 // Before it, unless the plan says `own`, launch_mx_input.  `g` holds the matrix, err, stamp and the outputs; launches: how many.
 cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st,
                               bool pdl, int *launches);
-cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st, bool pdl);
+// early: as in MxArgs; else the product is let start when all that came before this kernel is done.
+cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, bool early, cudaStream_t st, bool pdl);
 // bytes of 128 columns of the activations with `ncols` = planes x Mc instruction columns: elements, then scales
 __host__ __device__ inline int mx_x_block(int ncols) { return ncols * kMxTileK + 512 * ((ncols + 127) / 128); }
 

@@ -200,7 +200,8 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
       bulk_load(dst + kProdW + x_block, g.w + (size_t)blk * kMxTileBytes + kMxCodeBytes, 512, bar, pol_w);
     };
     auto load_x = [&](uint32_t dst, uint32_t bar, int blk) { bulk_load(dst + kProdW, (const uint8_t *)g.x + (size_t)blk * x_block, x_block, bar, pol_a); };
-    // weights do not depend on the previous kernel: they are on their way before the programmatic-dependency wait
+    // weights do not depend on the previous kernel, unless it laid them out: they are on their way before the programmatic-dependency wait
+    if (!g.early) pdl_wait();
     const int pre = min(g.stages, n);
     for (int pass = 0; pass < 2; ++pass) {
       long long hi = u1;

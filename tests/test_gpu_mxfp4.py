@@ -266,3 +266,89 @@ def test_quantise_lay_out_multiply_together():
     _check(y, x, ref.values(codes.cpu().numpy(), scales.cpu().numpy(), 2048), 2048, torch.float32)
     full = _f64(x) @ _f64(a).T
     assert np.linalg.norm(_f64(y) - full) < 0.25 * np.linalg.norm(full)
+
+
+def test_a_matrix_laid_out_just_before_is_read_as_laid_out():
+    """lay_out and product back to back, the same memory each time with another matrix: with one row (a launch that makes its own
+    planes) and with several, enough k-blocks for a ring to be filled at once."""
+    rng = np.random.default_rng(12)
+    n, k = 4096, 1024
+    packs = [(torch.from_numpy(rng.integers(0, 256, (n, k // 2), dtype=np.uint8)).cuda(), torch.full((n, k // 32), 120 + i, dtype=torch.uint8, device="cuda"))
+             for i in range(4)]
+    w = ts.Mxfp4Matrix(*packs[0], k)
+    fresh = [ts.Mxfp4Matrix(*p, k) for p in packs]
+    for m in (1, 2, 9, 40):
+        x = torch.randn(m, k, device="cuda").to(torch.bfloat16)
+        ws = w.workspace(m, x.dtype)
+        want = [ts.ts_mxfp4_product(f, x, torch.float32) for f in fresh]
+        got = []
+        for _ in range(10):
+            for p in packs:
+                ts.binding._check(ts.binding.lib().ts_mxfp4_lay_out(p[0].data_ptr(), p[1].data_ptr(), n, k, w.data.data_ptr(),
+                                                                     torch.cuda.current_stream().cuda_stream))
+                got.append(ts.ts_mxfp4_product(w, x, torch.float32, workspace=ws))
+        for i, y in enumerate(got):
+            assert torch.equal(y, want[i % 4]), (m, i)
+
+
+def test_products_on_two_streams_at_once():
+    rng = np.random.default_rng(13)
+    _, _, a = _weights(rng, 39000, 512)      # dealt out in runs: its CTAs wait for one another
+    _, _, b = _weights(rng, 39000, 512)
+    x = [torch.randn(20, 512, device="cuda") for _ in range(2)]
+    want = [ts.ts_mxfp4_product(w, v) for w, v in zip((a, b), x)]
+    streams, ws = [torch.cuda.Stream() for _ in range(2)], [w.workspace(20, torch.float32) for w in (a, b)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        for w, v, st, scratch in zip((a, b), x, streams, ws):
+            got.append(ts.ts_mxfp4_product(w, v, workspace=scratch, stream=st))
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+    for i, y in enumerate(got):
+        assert torch.equal(y, want[i % 2])
+
+
+def test_the_first_call_may_be_captured():
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2604_13519_b200 as ts
+x = torch.randn(3, 512, device="cuda").to(torch.bfloat16)
+codes, scales = torch.randint(0, 256, (640, 256), dtype=torch.uint8, device="cuda"), torch.full((640, 16), 120, dtype=torch.uint8, device="cuda")
+w = ts.Mxfp4Matrix(codes, scales, 512)
+ws = w.workspace(3, x.dtype)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    y, one = ts.ts_mxfp4_product(w, x, workspace=ws), ts.ts_mxfp4_product(w, x[:1], workspace=ws)
+    v = ts.ts_mxfp4_dequantise(*ts.ts_mxfp4_quantise(x), 512, torch.float32)
+g.replay()
+w.check()
+assert torch.equal(y, ts.ts_mxfp4_product(w, x)) and torch.equal(one, y[:1])
+assert torch.equal(v, ts.ts_mxfp4_dequantise(*ts.ts_mxfp4_quantise(x), 512, torch.float32))
+print("captured")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+def test_refusals_on_the_device():
+    _, _, w = _weights(np.random.default_rng(14), 200, 64)
+    x = torch.randn(20, 64, device="cuda")
+    ws = w.workspace(20, x.dtype)
+    full = torch.zeros(20, 200, device="cuda")
+    for bad in (dict(workspace=ws[:64]), dict(workspace=ws[1:]), dict(workspace=ws.cpu()), dict(out=full[:19]), dict(out=full, dtype=torch.float16),
+                dict(out=full.t().contiguous().t())):
+        with pytest.raises((ts.TsError, ValueError)):
+            ts.ts_mxfp4_product(w, x, **bad)
+    for bad in (x[:, :32], x.t(), x.double(), x.cpu(), x[None]):
+        with pytest.raises((ValueError, TypeError)):
+            ts.ts_mxfp4_product(w, bad)
+    codes, scales = ts.ts_mxfp4_quantise(x)
+    for c, s, cols in ((codes[:, :16], scales, 64), (codes, scales[:5], 64), (codes, scales, 65), (codes.cpu(), scales, 64)):
+        with pytest.raises(ValueError):
+            ts.ts_mxfp4_dequantise(c, s, cols, torch.float32)
