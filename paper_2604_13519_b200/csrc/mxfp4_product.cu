@@ -23,10 +23,10 @@
 // Otherwise one tile to a CTA, or, where that leaves places empty, to a cluster of CTAs along K, whose sums meet through
 // distributed shared memory: less of an exchange than through L2, which counts where a CTA has few k-blocks.
 //
-// Up to two rows the CTAs of the second kind make the planes themselves (kOwn): four more warps turn a stage's 128 columns into e4m3
+// Up to two or four rows the CTAs of the second kind make the planes themselves (kOwn): four more warps turn a stage's 128 columns into e4m3
 // on the way into shared memory, which saves a launch; for more rows a kernel ahead does it once for all CTAs (launch_mx_planes8).
 //
-// Roles: warp 0 = copies, warp 1 = tensor memory, scales and products, warps 2..5 = epilogue, warps 6..9 = planes (kOwn).
+// Roles: warp 0 = copies, warp 1 = tensor memory, scales and products, warps 2..5 = epilogue, warps 6.. = planes (kOwn).
 // Every wait is bounded; on expiry the CTA records an error word and leaves through the normal exit.
 #include <cuda_fp16.h>
 
@@ -144,8 +144,10 @@ __device__ __forceinline__ void prod_sums(const MxArgs &g, uint32_t taddr, float
     }
 }
 
-template <int EPI, bool kStream, bool kOwn, int TYPE>
-__global__ void __launch_bounds__(kOwn ? 320 : 192, kProdCtas)
+// kOwn: pairs of rows whose planes the CTA makes, 0: none
+__host__ __device__ constexpr int own_warps(int own) { return own == 0 ? 0 : 4; }
+template <int EPI, bool kStream, int kOwn, int TYPE>
+__global__ void __launch_bounds__(192 + 32 * own_warps(kOwn), kProdCtas)
 mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const int ncols = g.planes * g.Mc, sb_words = (ncols + 127) / 128;   // (512 bytes of scales for 128 columns)
@@ -427,39 +429,41 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
       }
       mx_finish<EPI>(g, g.row0 + m0 + m, n, v, lane);
     }
-  } else if (kOwn) {
+  } else if constexpr (kOwn > 0) {
     // ------------------------------------------------------------------ planes
-    // A warp to a block, four blocks at a time (one block's chain of conversions takes about a thousand cycles): sixteen threads to a row,
-    // eight columns each.
+    // A warp to a block, as many blocks at a time as there are warps (one block's chain of conversions takes about a thousand cycles):
+    // sixteen threads to a row, eight columns each, two rows at a time.
     typedef typename MxElem<TYPE>::raw raw;
-    constexpr int kWarps = 4, kAhead = 2;   // a warp's blocks whose columns are on their way
-    const int m = lane >> 4, col = (lane & 15) * 8, kb0 = (int)(u0 - first), nkb = (int)(u1 - u0);
-    const bool there = m < g.M;
-    const raw *row = (const raw *)g.x + (size_t)m * g.ldx;
-    pdl_wait();
-    MxRaw8<TYPE> x[kAhead];
-    int i = warp - 6;
+    // (no more warps than stages: a warp that has a block's stage has seen the stage of the block `warps` before emptied, so that the parity
+    // it waits for is never that of a phase long past)
+    const int warps = min(own_warps(kOwn), g.stages);
+    const int col = (lane & 15) * 8, kb0 = (int)(u0 - first), nkb = (int)(u1 - u0);
+    MxRaw8<TYPE> x[kOwn];   // the warp's next block
+    auto fetch = [&](int i) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) mx_fetch8<TYPE>(row, g.pair, there && i + j * kWarps < nkb, (kb0 + i + j * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
-    for (bool ok = true; ok && i < nkb;) {
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        if (!ok || i >= nkb) break;
-        float v[8];
-        mx_widen8<TYPE>(x[j], v);
-        mx_fetch8<TYPE>(row, g.pair, there && i + kAhead * kWarps < nkb, (kb0 + i + kAhead * kWarps) * kMxTileK + col, g.K, g.vec_x, x[j]);
-        const int s = i % g.stages;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->empty[s]), ((i / g.stages) & 1) ^ 1));
-        if (!ok) {
-          if (lane == 0) prod_error(g, DEV_TIMEOUT_EMPTY);
-          break;
-        }
-        mx_to_planes(v, there, smem + (size_t)s * stage_bytes + kProdW, act_bytes, g.Mc, g.planes, m, col);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ctl->full[s]));
-        i += kWarps;
+      for (int r = 0; r < kOwn; ++r) {
+        const int m = 2 * r + (lane >> 4);
+        mx_fetch8<TYPE>((const raw *)g.x + (size_t)m * g.ldx, g.pair, m < g.M && i < nkb, (kb0 + i) * kMxTileK + col, g.K, g.vec_x, x[r]);
       }
+    };
+    pdl_wait();
+    if (warp - 6 < warps) fetch(warp - 6);
+    for (int i = warp - 6; warp - 6 < warps && i < nkb; i += warps) {
+      float v[kOwn][8];
+#pragma unroll
+      for (int r = 0; r < kOwn; ++r) mx_widen8<TYPE>(x[r], v[r]);
+      fetch(i + warps);
+      const int s = i % g.stages;
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->empty[s]), ((i / g.stages) & 1) ^ 1))) {
+        if (lane == 0) prod_error(g, DEV_TIMEOUT_EMPTY);
+        break;
+      }
+#pragma unroll
+      for (int r = 0; r < kOwn; ++r)
+        if (2 * r < g.M) mx_to_planes(v[r], 2 * r + (lane >> 4) < g.M, smem + (size_t)s * stage_bytes + kProdW, act_bytes, g.Mc, g.planes, 2 * r + (lane >> 4), col);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ctl->full[s]));
     }
   }
   if constexpr (!kStream) {
@@ -498,7 +502,9 @@ static size_t prod_stage_bytes(int planes, int Mc) {
 // second exchange at a run's end, 7 to 12 us.  An SM takes a block in about 256 + 2 x columns cycles, the time of its bytes through shared
 // memory (weights 16 KB, columns x 128, all of it written and read, 128 a cycle).  301 rows of fp16 x 4096 x 12288, 160 tiles: 66 -> 63 us;
 // 64 rows x 24576 x 4096, 192 tiles: 21 us and 28 in runs, 112 rows 31 and 39.
-constexpr int kOwnRows = 2;     // most rows whose planes the product makes itself
+// Rows whose planes the product makes itself: up to two, and up to four where a CTA has few blocks (its warps make a block of four rows in
+// about as long as a block of two takes to be multiplied; 4096 x 4096 at 4 rows 8.4 -> 7.4 us, 24576 x 4096 at 3 rows 15.4 and 17.1).
+constexpr int kOwnRows = 2, kOwnRowsShort = 4, kOwnShort = 8;
 constexpr int kRunCycles = 25000;
 MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits) {
   MxPlan p{};
@@ -518,7 +524,7 @@ MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fit
   for (int c = 2; fits && !p.stream && c <= 8 && c <= n_kb; ++c)
     if (fits[c] * 10ll >= items * 11) p.cluster = c;
   p.ctas = (int)(p.stream ? places : (long long)tiles * p.chunks);
-  p.own = !p.stream && M <= kOwnRows;
+  p.own = !p.stream && M <= (n_kb <= kOwnShort * p.cluster ? kOwnRowsShort : kOwnRows);
   return p;
 }
 
@@ -547,7 +553,7 @@ void mx_fits(int (&fits)[9]) {
   for (int c = 1; c <= 8; ++c) fits[c] = gemm_max_clusters(c, 113 * 1024);
 }
 
-template <int EPI, bool kStream, bool kOwn, int TYPE>
+template <int EPI, bool kStream, int kOwn, int TYPE>
 static cudaError_t prod_launch_one(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
   static PerDeviceOnce once;
   int dev = -1;
@@ -558,7 +564,7 @@ static cudaError_t prod_launch_one(const CUtensorMap &tw, const MxArgs &g, const
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(p.ctas, p.cluster);
-  cfg.blockDim = dim3(kOwn ? 320 : 192);
+  cfg.blockDim = dim3(192 + 32 * own_warps(kOwn));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
@@ -580,15 +586,19 @@ static cudaError_t prod_launch_one(const CUtensorMap &tw, const MxArgs &g, const
   return cudaLaunchKernelEx(&cfg, mx_product_kernel<EPI, kStream, kOwn, TYPE>, tw, g);
 }
 
+template <int EPI, int TYPE>
+static cudaError_t prod_launch_own(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
+  return g.M <= 2 ? prod_launch_one<EPI, false, 1, TYPE>(tw, g, p, smem, st, pdl) : prod_launch_one<EPI, false, 2, TYPE>(tw, g, p, smem, st, pdl);
+}
 template <int EPI>
 static cudaError_t prod_launch(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
-  if (p.stream) return prod_launch_one<EPI, true, false, 0>(tw, g, p, smem, st, pdl);
-  if (!p.own) return prod_launch_one<EPI, false, false, 0>(tw, g, p, smem, st, pdl);
+  if (p.stream) return prod_launch_one<EPI, true, 0, 0>(tw, g, p, smem, st, pdl);
+  if (!p.own) return prod_launch_one<EPI, false, 0, 0>(tw, g, p, smem, st, pdl);
   switch (g.x_type) {
-    case MX_BF16: return prod_launch_one<EPI, false, true, MX_BF16>(tw, g, p, smem, st, pdl);
-    case MX_F16: return prod_launch_one<EPI, false, true, MX_F16>(tw, g, p, smem, st, pdl);
-    case MX_PAIR: return prod_launch_one<EPI, false, true, MX_PAIR>(tw, g, p, smem, st, pdl);
-    default: return prod_launch_one<EPI, false, true, MX_F32>(tw, g, p, smem, st, pdl);
+    case MX_BF16: return prod_launch_own<EPI, MX_BF16>(tw, g, p, smem, st, pdl);
+    case MX_F16: return prod_launch_own<EPI, MX_F16>(tw, g, p, smem, st, pdl);
+    case MX_PAIR: return prod_launch_own<EPI, MX_PAIR>(tw, g, p, smem, st, pdl);
+    default: return prod_launch_own<EPI, MX_F32>(tw, g, p, smem, st, pdl);
   }
 }
 

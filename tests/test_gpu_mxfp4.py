@@ -352,3 +352,17 @@ def test_refusals_on_the_device():
     for c, s, cols in ((codes[:, :16], scales, 64), (codes, scales[:5], 64), (codes, scales, 65), (codes.cpu(), scales, 64)):
         with pytest.raises(ValueError):
             ts.ts_mxfp4_dequantise(c, s, cols, torch.float32)
+
+
+@pytest.mark.parametrize("x_type", TYPES)
+def test_few_rows_many_times(x_type):
+    """One to eight rows over matrices of many k-blocks, the ring several times full: every call the same result."""
+    rng = np.random.default_rng(15)
+    for n, k in ((6144, 4096), (24576, 1024), (128, 12288)):
+        _, _, w = _weights(rng, n, k)
+        x = torch.randn(64, k, device="cuda").to(TYPES[x_type])
+        whole = ts.ts_mxfp4_product(w, x[:32], torch.float32)
+        for m in (1, 2, 3, 5, 8):
+            for _ in range(20):
+                assert torch.equal(ts.ts_mxfp4_product(w, x[:m], torch.float32), whole[:m]), (n, k, m)
+        w.check()
