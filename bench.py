@@ -143,12 +143,12 @@ def get_workload(name):
     return WORKLOADS[name]
 
 
-def algorithmic_bytes(shape, lens, ks):
+def algorithmic_bytes(shape, lens, ks, weights_held="bf16"):
     """Bytes one verify step must move: every weight matrix once, the context K/V once, the chunk's
     K/V written, the logits written, the embedding rows read (the embedding table itself is not)."""
     s = shape
     M = sum(ks)
-    weights = 2 * s.n_params_matmul()
+    weights = 2 * s.n_params_matmul() if weights_held == "bf16" else s.n_params_matmul() * 17 // 32
     kv_read = sum(lens) * 4 * s.n_kv_heads * s.head_dim * s.n_layers
     kv_write = M * 4 * s.n_kv_heads * s.head_dim * s.n_layers
     return dict(weights=weights, kv_read=kv_read, kv_write=kv_write, logits=4 * M * s.vocab,
@@ -581,7 +581,7 @@ def main():
             a[0] += pm / 3
             a[1] = pn
     peaks = measured_peaks()
-    ab = algorithmic_bytes(shape, lens, ks)
+    ab = algorithmic_bytes(shape, lens, ks, args.weights)
     fl = algorithmic_flops(shape, lens, ks)
     t_hbm = ab["total"] / (peaks["hbm_gbs"] * 1e9)
     t_tc = fl / (peaks["bf16_tflops"] * 1e12)
@@ -646,6 +646,8 @@ def main():
                "sample": f"one chunk forward over the first {nl} of {shape.n_layers} layers + LM head on the same "
                          f"shapes, layer time scaled to full depth ({sec:.1f} s per step)"}
 
+    if args.weights != "bf16":
+        roofline = None     # (of the bf16 projections' kernel)
     if rank == 0:
         out = {
             "metric": METRIC, "value": world * M / (ms * 1e-3), "unit": UNIT, "n_gpus": world, "steps": args.steps,
@@ -653,7 +655,8 @@ def main():
             "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
             "config": {"workload": args.workload, "batch": len(lens), "context": lens, "k": ks,
                        "act_split": planes == 2, "draft_tree": bool(args.tree), "temperature": args.temperature, "per_position_topk": bool(args.want_topk), "kv_dtype": "f16", "l2": "inputs (weights) far larger than L2",
-                       "parallelism": "replicas" if world > 1 else "single"},
+                       "parallelism": "replicas" if world > 1 else "single",
+                       **({} if args.weights == "bf16" else {"weights": args.weights})},
             "latency_ms": {"p50": statistics.median(lat), "p90": sorted(lat)[int(0.9 * (len(lat) - 1))]},
             "clocks": clocks,
             "e2e": {"value": world * M / (e2e_ms * 1e-3), "unit": UNIT, "ms_per_step": e2e_ms,

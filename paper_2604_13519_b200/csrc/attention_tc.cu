@@ -30,6 +30,7 @@
 #include <algorithm>
 
 #include "kernels.h"
+#include "mxfp4.h"
 #include "schedule.h"
 
 namespace ts {
@@ -575,7 +576,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 // every lane loads its elements of all slots at once (one round trip to L2, 16 bytes per lane and slot) and adds them in
 // slot order.  NS = compile-time bound on the number of slots.  (RW > 1 for many rows, where a row at a time is several
 // waves of CTAs that each wait for a few round trips: 1024 rows of the 8B shape 29 us, four at a time 9.5.)
-template <int NS, int VW, int RW>
+template <int NS, int VW, int RW, bool MX>
 __global__ void __launch_bounds__(128) attn_merge_kernel(const AttnTcArgs a) {
   if (threadIdx.x == 0) stamp_min(a.stamp_merge);
   pdl_launch_dependents();   // the dependent kernel waits for this one's end before touching its data
@@ -594,6 +595,7 @@ __global__ void __launch_bounds__(128) attn_merge_kernel(const AttnTcArgs a) {
   }
   pdl_wait();
   if (threadIdx.x == 0) stamp_waited(a.stamp_merge);
+  if (MX && blockIdx.x == 0 && blockIdx.y == 0) mx_clear_flags(a.mo, threadIdx.x, blockDim.x);
   if (h >= a.Hq) return;
   float2 ml[RW];
   float t[RW][NS][VW];
@@ -648,6 +650,7 @@ __global__ void __launch_bounds__(128) attn_merge_kernel(const AttnTcArgs a) {
       *reinterpret_cast<uint32_t *>(o_hi) = *reinterpret_cast<const uint32_t *>(hi);
       if (a.planes == 2) *reinterpret_cast<uint32_t *>(o_lo) = *reinterpret_cast<const uint32_t *>(lo);
     }
+    if constexpr (MX) mx_put<VW>(a.mo, m, (int)col, hi, lo, a.planes);
   }
   if (threadIdx.x == 0 && a.stamp_merge) stamp_max(a.stamp_merge + 3);
 }
@@ -663,7 +666,7 @@ static cudaError_t launch_merge_pdl(const AttnTcArgs &a, cudaStream_t st) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attn_merge_kernel<NS, VW, RW>, a);
+  return a.mo.out ? cudaLaunchKernelEx(&cfg, attn_merge_kernel<NS, VW, RW, true>, a) : cudaLaunchKernelEx(&cfg, attn_merge_kernel<NS, VW, RW, false>, a);
 }
 
 template <int VW>

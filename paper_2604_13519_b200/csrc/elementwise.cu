@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "kernels.h"
+#include "mxfp4.h"
 
 namespace ts {
 
@@ -28,11 +29,12 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
 // registers across the block reduction, so that nothing is read back.  (Spreading a row over a cluster of CTAs with
 // the sums of squares exchanged through distributed shared memory was measured and is not faster: the kernel's time
 // is the latency of its first access after the wait and of its exit, not the bytes one SM pulls from L2.)
-template <int MODE>
+// MX: the planes once more for an MXFP4 product.
+template <int MODE, bool MX>
 __global__ void __launch_bounds__(kNormMaxThreads)
 norm_kernel(const int32_t *tokens, const __nv_bfloat16 *embed, const float *part, int n_splits, int part_rows,
             const float *gain, float eps, int d, float *x, __nv_bfloat16 *h, int h_rows, int planes,
-            unsigned long long *amax, unsigned long long *stamp, BoundsCheck bc) {
+            unsigned long long *amax, unsigned long long *stamp, BoundsCheck bc, MxOut mo) {
   __shared__ float red[32];
   if (threadIdx.x == 0) stamp_min(stamp);
   pdl_launch_dependents();   // the dependent kernel waits for this one's end before touching its data
@@ -47,6 +49,7 @@ norm_kernel(const int32_t *tokens, const __nv_bfloat16 *embed, const float *part
   float ss = 0.f;
   float4 keep = make_float4(0.f, 0.f, 0.f, 0.f);
   if (MODE == 0 && threadIdx.x == 0) amax[(size_t)m * kAmaxStride] = 0ull;
+  if (MX && m == 0) mx_clear_flags(mo, threadIdx.x, blockDim.x);
   for (int c = c0; c < d; c += blockDim.x * 4) {
     float4 v;
     if (MODE == 0) {
@@ -95,6 +98,7 @@ norm_kernel(const int32_t *tokens, const __nv_bfloat16 *embed, const float *part
     for (int j = 0; j < 4; ++j) split_bf16(o[j], hi[j], lo[j]);
     *reinterpret_cast<uint2 *>(h + (size_t)m * d + c) = *reinterpret_cast<uint2 *>(hi);
     if (planes == 2) *reinterpret_cast<uint2 *>(h + ((size_t)h_rows + m) * d + c) = *reinterpret_cast<uint2 *>(lo);
+    if constexpr (MX) mx_put<4>(mo, m, c, hi, lo, planes);   // (d is a multiple of 128: a warp is in the row or behind it)
   }
   if (stamp) { __syncthreads(); if (threadIdx.x == 0) stamp_max(stamp + 3); }
 }
@@ -105,10 +109,10 @@ norm_kernel(const int32_t *tokens, const __nv_bfloat16 *embed, const float *part
 static constexpr int kNormRowsThreads = 256;
 static constexpr int kNormChunks = 4;      // d <= 4096; a wider row and its slabs would not fit the registers of two CTAs per SM, and takes
                                            // the form above (not tried otherwise)
-template <int NS>   // most slabs: all loads are issued before the first sum
+template <int NS, bool MX>   // NS, most slabs: all loads are issued before the first sum
 __global__ void __launch_bounds__(kNormRowsThreads, NS == 1 ? 5 : NS == 2 ? 4 : NS == 3 ? 3 : 2)
 norm_rows_kernel(const float *part, int n_splits, int part_rows, const float *gain, float eps, int d, float *x,
-                 __nv_bfloat16 *h, int h_rows, int planes, unsigned long long *stamp) {
+                 __nv_bfloat16 *h, int h_rows, int planes, unsigned long long *stamp, MxOut mo) {
   __shared__ float red[32];
   if (threadIdx.x == 0) stamp_min(stamp);
   pdl_launch_dependents();   // the dependent kernel waits for this one's end before touching its data
@@ -153,8 +157,10 @@ norm_rows_kernel(const float *part, int n_splits, int part_rows, const float *ga
       for (int j = 0; j < 4; ++j) split_bf16(o[j], hi[j], lo[j]);
       *reinterpret_cast<uint2 *>(h + (size_t)m * d + c) = *reinterpret_cast<uint2 *>(hi);
       if (planes == 2) *reinterpret_cast<uint2 *>(h + ((size_t)h_rows + m) * d + c) = *reinterpret_cast<uint2 *>(lo);
+      if constexpr (MX) mx_put<4>(mo, m, c, hi, lo, planes);
     }
   }
+  if (MX && m == 0) mx_clear_flags(mo, threadIdx.x, blockDim.x);
   if (stamp) { __syncthreads(); if (threadIdx.x == 0) stamp_max(stamp + 3); }
 }
 
@@ -178,21 +184,21 @@ static int norm_threads(int d) { return std::min(kNormMaxThreads, (d / 4 + 31) /
 
 cudaError_t launch_embed_norm(const StepIn &in, const __nv_bfloat16 *embed, const float *gain, float eps,
                               int d, float *x, __nv_bfloat16 *h, int h_rows, int planes,
-                              unsigned long long *amax, cudaStream_t st) {
-  return launch_pdl(norm_kernel<0>, dim3(in.M), dim3(norm_threads(d)), 0, st, in.tokens, embed,
-                    (const float *)nullptr, 0, 0, gain, eps, d, x, h, h_rows, planes, amax, (unsigned long long *)nullptr, in.ck);
+                              unsigned long long *amax, const MxOut &mo, cudaStream_t st) {
+  return launch_pdl(mo.out ? norm_kernel<0, true> : norm_kernel<0, false>, dim3(in.M), dim3(norm_threads(d)), 0, st, in.tokens, embed,
+                    (const float *)nullptr, 0, 0, gain, eps, d, x, h, h_rows, planes, amax, (unsigned long long *)nullptr, in.ck, mo);
 }
 
 cudaError_t launch_add_norm(int M, int d, const float *part, int n_splits, int part_rows, const float *gain,
-                            float eps, float *x, __nv_bfloat16 *h, int h_rows, int planes, cudaStream_t st,
+                            float eps, float *x, __nv_bfloat16 *h, int h_rows, int planes, const MxOut &mo, cudaStream_t st,
                             unsigned long long *stamp) {
-  if (n_splits > kNormMaxSplits) return cudaErrorInvalidValue;
+  if (n_splits > kNormMaxSplits || (mo.out && n_splits > 1)) return cudaErrorInvalidValue;
   if (M >= kNormManyRows && d <= kNormChunks * 4 * kNormRowsThreads && n_splits <= 4)
-    return launch_pdl(n_splits <= 1 ? norm_rows_kernel<1> : n_splits <= 2 ? norm_rows_kernel<2> : n_splits <= 3 ? norm_rows_kernel<3> : norm_rows_kernel<4>, dim3(M), dim3(kNormRowsThreads), 0, st, part, n_splits, part_rows, gain, eps, d, x,
-                      h, h_rows, planes, stamp);
-  return launch_pdl(norm_kernel<1>, dim3(M), dim3(norm_threads(d)), 0, st, (const int32_t *)nullptr,
+    return launch_pdl(mo.out ? norm_rows_kernel<1, true> : n_splits <= 1 ? norm_rows_kernel<1, false> : n_splits <= 2 ? norm_rows_kernel<2, false> : n_splits <= 3 ? norm_rows_kernel<3, false> : norm_rows_kernel<4, false>,
+                      dim3(M), dim3(kNormRowsThreads), 0, st, part, n_splits, part_rows, gain, eps, d, x, h, h_rows, planes, stamp, mo);
+  return launch_pdl(mo.out ? norm_kernel<1, true> : norm_kernel<1, false>, dim3(M), dim3(norm_threads(d)), 0, st, (const int32_t *)nullptr,
                     (const __nv_bfloat16 *)nullptr, part, n_splits, part_rows, gain, eps, d, x, h, h_rows,
-                    planes, (unsigned long long *)nullptr, stamp, BoundsCheck{});
+                    planes, (unsigned long long *)nullptr, stamp, BoundsCheck{}, mo);
 }
 
 __device__ __forceinline__ __half to_half_sat(float x) {

@@ -98,13 +98,22 @@ int gemm_rows_tiles(int N);
 cudaError_t launch_gemm_rows(int epi, const CUtensorMap &tw, const CUtensorMap &ta, GemmArgs g, int n_splits,
                              size_t smem_limit, int n_sms, cudaStream_t st, bool pdl);
 
+// Where a kernel also leaves its output as the planes of e4m3 numbers that a product with an MXFP4 matrix reads (mxfp4.h), instead of a kernel
+// of the product's own that reads the bf16 planes back (4 us each in a step of 32 rows).  Null out: not wanted.
+struct MxOut {
+  uint8_t *out;
+  int Mc, planes, n_kb;   // rows per chunk, planes, 128-column blocks of a row
+  int *flags;             // cleared
+  int n_flags;
+};
+
 // x[m] = E[tokens[m]]; h = rmsnorm(x) * gain -> bf16 (hi[, lo])
 cudaError_t launch_embed_norm(const StepIn &in, const __nv_bfloat16 *embed, const float *gain, float eps,
                               int d, float *x, __nv_bfloat16 *h, int h_rows, int planes,
-                              unsigned long long *amax, cudaStream_t st);
+                              unsigned long long *amax, const MxOut &mo, cudaStream_t st);
 // x[m] += sum_s part[s][m]; h = rmsnorm(x) * gain -> bf16 (hi[, lo])
 cudaError_t launch_add_norm(int M, int d, const float *part, int n_splits, int part_rows, const float *gain,
-                            float eps, float *x, __nv_bfloat16 *h, int h_rows, int planes, cudaStream_t st,
+                            float eps, float *x, __nv_bfloat16 *h, int h_rows, int planes, const MxOut &mo, cudaStream_t st,
                             unsigned long long *stamp = nullptr);
 // qkv = sum of split-K partials; rotary on q and k; q -> fp16 [M][Hq][hd] and the rounding remainder of
 // every element as a second array of the same shape; k, v -> fp16 pages
@@ -160,6 +169,7 @@ struct AttnTcArgs {
   int out_rows, planes;
   int *err;                      // device status word
   unsigned long long *stamp, *stamp_merge;   // optional clock stamps of the attention and the merge launch
+  MxOut mo;                      // the merged rows once more
 };
 cudaError_t launch_attention_tc(const AttnTcArgs &a, cudaStream_t st);
 cudaError_t launch_attention_tc_merge(const AttnTcArgs &a, cudaStream_t st);

@@ -86,7 +86,7 @@ struct Layout {
   int n_maps, n_counters, n_phases;
   StepIo step_io, prompt_io;   // of a verification step, of a piece of a prompt
   int in_ints, o_path, o_topk;
-  uint64_t samp_stats, topk_cand, mx;
+  uint64_t samp_stats, topk_cand, mx, mx2;
   // step out (int32 offsets)
   int o_argmax, o_accept, o_emitted, o_newlen, o_newpend, o_err, o_done, out_ints;
   int rows_alloc;        // rows of the activation buffers: max_rows or a piece of a prompt, whichever is more
@@ -219,9 +219,12 @@ void make_layout(const ts_model_config &c, Layout *L) {
   L->phase_t = take((uint64_t)3 * L->n_phases * 8);
   L->max_stamps = 18 * c.n_layers + 16;   // (launches of a step: 9 per layer, in MXFP4 13, or 17 where rows go in two passes)
   L->stamps = take((uint64_t)L->max_stamps * 4 * 8);
-  L->mx = 0;
-  if (c.weights == TS_WEIGHTS_MXFP4)   // planes of the activations, sums of tiles that two CTAs share
-    L->mx = take(ts::mx_scratch_most((int)R, (int)((std::max(std::max(d, F), Nq) + ts::kMxTileK - 1) / ts::kMxTileK), ts::mx_planes_of(c.act_split ? ts::MX_PAIR : ts::MX_BF16)));
+  L->mx = L->mx2 = 0;
+  if (c.weights == TS_WEIGHTS_MXFP4) {   // planes of the projections' inputs (of `down` apart), sums of tiles that two CTAs share
+    const int planes_mx = ts::mx_planes_of(c.act_split ? ts::MX_PAIR : ts::MX_BF16);
+    L->mx = take(ts::mx_scratch_most((int)R, (int)((std::max(d, Nq) + ts::kMxTileK - 1) / ts::kMxTileK), planes_mx));
+    L->mx2 = take(ts::mx_scratch_most((int)R, (int)((F + ts::kMxTileK - 1) / ts::kMxTileK), planes_mx));
+  }
   L->workspace_bytes = o;
   L->host_io_bytes = align_up((uint64_t)(L->in_ints + L->out_ints + 2 * ts::kTopMax + 2) * 4, 4096);   // (and a retrieval's result pairs, status and number)
 }
@@ -438,26 +441,37 @@ ts_status run_gemm_ws(ts_model *m, int epi, const CUtensorMap &tw, const CUtenso
   return TS_OK;
 }
 
-// A projection with an MXFP4 matrix: its input as planes of e4m3 numbers, then the product (mxfp4_product.cu).  x: bf16 planes [planes][R][K].
-ts_status run_mx(ts_model *m, int epi, const CUtensorMap &tw, uint64_t w, int N, int K, int M, const __nv_bfloat16 *x, float *out,
-                 __nv_bfloat16 *act_out, unsigned long long *amax) {
+// A projection with an MXFP4 matrix (mxfp4_product.cu): its plan, and where what makes its input leaves that as planes of e4m3 numbers (the input of
+// `down` apart from the others, since gate-up reads its own while it writes that).
+ts::MxPlan mx_plan_of(const ts_model *m, int N, int K, int M) {
+  return ts::mx_plan(M, N / ts::kMxTileN, (K + ts::kMxTileK - 1) / ts::kMxTileK, m->planes == 2 ? ts::mx_planes_of(ts::MX_PAIR) : ts::mx_planes_of(ts::MX_BF16),
+                     m->n_sms, m->max_clusters);
+}
+ts::MxOut mx_out_of(const ts_model *m, int N, int K, int M, uint64_t scratch) {
+  if (m->c.weights != TS_WEIGHTS_MXFP4 || K % ts::kMxTileK) return ts::MxOut{};   // (a last block with nothing in its second half: launch_mx_input fills it)
+  return ts::mx_out((K + ts::kMxTileK - 1) / ts::kMxTileK, m->planes == 2 ? ts::mx_planes_of(ts::MX_PAIR) : ts::mx_planes_of(ts::MX_BF16), m->WS(scratch),
+                    mx_plan_of(m, N, K, M));
+}
+// x: the input as bf16 planes [planes][R][K] (read by a product of few rows); there: the planes of e4m3 numbers are in the scratch memory.
+ts_status run_mx(ts_model *m, int epi, const CUtensorMap &tw, uint64_t w, int N, int K, int M, const __nv_bfloat16 *x, uint64_t scratch, bool there,
+                 float *out, __nv_bfloat16 *act_out, unsigned long long *amax, const ts::MxOut &mo) {
   const Layout &L = m->L;
   ts::MxArgs g{};
   g.w = m->W(w); g.N = N; g.tiles = N / ts::kMxTileN; g.n_kb = (K + ts::kMxTileK - 1) / ts::kMxTileK;
   g.err = m->d_out() + L.o_err;
   g.early = 1;
   g.y = out; g.ldy = N; g.y_type = ts::MX_F32; g.vec = 1;
-  g.out = out; g.act_out = act_out; g.act_rows = L.rows_alloc; g.out_planes = m->planes; g.amax = amax;
+  g.out = out; g.act_out = act_out; g.act_rows = L.rows_alloc; g.out_planes = m->planes; g.amax = amax; g.mo = mo;
   const ts::MxInput in{x, m->planes == 2 ? ts::MX_PAIR : ts::MX_BF16, M, K, K, (long long)L.rows_alloc * K};
-  const ts::MxPlan p = ts::mx_plan(M, g.tiles, g.n_kb, ts::mx_planes_of(in.type), m->n_sms, m->max_clusters);
+  const ts::MxPlan p = mx_plan_of(m, N, K, M);
   const bool pdl = m->use_pdl && !m->profiling;
-  if (!p.own) {
-    CU_TRY(ts::launch_mx_input(in, m->WS(L.mx), p, true, m->st, pdl));
+  if (!p.own && (!there || K % ts::kMxTileK)) {
+    CU_TRY(ts::launch_mx_input(in, m->WS(scratch), p, true, m->st, pdl));
     m->launched(0);
   }
   g.stamp = m->stamp_slot();
   int n = 0;
-  CU_TRY(ts::launch_mx_product(epi, tw, g, in, m->WS(L.mx), p, m->st, pdl, &n));
+  CU_TRY(ts::launch_mx_product(epi, tw, g, in, m->WS(scratch), p, m->st, pdl, &n));
   for (int i = 0; i < n; ++i) m->launched(0);
   return TS_OK;
 }
@@ -576,8 +590,9 @@ ts_status run_step(ts_model *m) {
   at.q = q; at.q_lo = q + (size_t)R * Nq; at.map_kv = (const CUtensorMap *)m->WS(L.maps) + (L.n_maps - 1);
   at.attn_o = aa.part_o; at.attn_ml = aa.part_ml; at.err = m->d_out() + L.o_err;
   at.out = attn; at.out_rows = R; at.planes = m->planes;
+  at.mo = mx_out_of(m, d, Nq, M, L.mx);
   CU_TRY(ts::launch_embed_norm(in, (const __nv_bfloat16 *)m->W(L.embed), (const float *)m->W(L.g1[0]), c.rms_eps,
-                               d, x, h, R, m->planes, (unsigned long long *)m->WS(L.amax), m->st));
+                               d, x, h, R, m->planes, (unsigned long long *)m->WS(L.amax), mx_out_of(m, L.Nqkv, d, M, L.mx), m->st));
   m->launched(3);
   // Up to kFewRows rows the weight-streaming kernel: QKV rotates and appends K/V itself, O and down update the residual stream
   // and prepare the next projection's input (6 launches per layer); beyond, the many-rows kernel with its split-K slabs
@@ -600,11 +615,11 @@ ts_status run_step(ts_model *m) {
     } else {
       if (l > 0) {
         CU_TRY(ts::launch_add_norm(M, d, part, splits, part_R, (const float *)m->W(L.g1[l]), c.rms_eps, x, h, R,
-                                   m->planes, m->st, m->stamp_slot()));
+                                   m->planes, mx_out_of(m, L.Nqkv, d, M, L.mx), m->st, m->stamp_slot()));
         m->launched(3);
       }
       splits = 1;
-      s = mx ? run_mx(m, ts::MX_STORE, m->tm_qkv[l], L.wqkv[l], L.Nqkv, d, M, h, part, nullptr, nullptr)
+      s = mx ? run_mx(m, ts::MX_STORE, m->tm_qkv[l], L.wqkv[l], L.Nqkv, d, M, h, L.mx, true, part, nullptr, nullptr, ts::MxOut{})
              : run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_qkv[l], m->tm_h, L.Nqkv, d, M, part, nullptr, nullptr, &splits);
       if (s) return s;
       CU_TRY(ts::launch_rope_kv(in, part, splits, part_R, c.n_q_heads, c.n_kv_heads, c.head_dim, rope, q,
@@ -644,24 +659,24 @@ ts_status run_step(ts_model *m) {
       s = run_gemm_ws(m, ts::EPI_RESID, m->tm_d[l], m->tm_act, d, F, M, g);
       if (s) return s;
     } else {
-      s = mx ? run_mx(m, ts::MX_STORE, m->tm_o[l], L.wo[l], d, Nq, M, attn, part, nullptr, nullptr)
+      s = mx ? run_mx(m, ts::MX_STORE, m->tm_o[l], L.wo[l], d, Nq, M, attn, L.mx, m->fused_ok, part, nullptr, nullptr, ts::MxOut{})
              : run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_o[l], m->tm_attn, d, Nq, M, part, nullptr, nullptr, &splits);
       if (s) return s;
       CU_TRY(ts::launch_add_norm(M, d, part, splits, part_R, (const float *)m->W(L.g2[l]), c.rms_eps, x, h, R,
-                                 m->planes, m->st, m->stamp_slot()));
+                                 m->planes, mx_out_of(m, 2 * F, d, M, L.mx), m->st, m->stamp_slot()));
       m->launched(3);
       // (gate-up keeps its SwiGLU epilogue and so cannot split K)
-      s = mx ? run_mx(m, ts::MX_SWIGLU, m->tm_gu[l], L.wgu[l], 2 * F, d, M, h, nullptr, act, nullptr)
+      s = mx ? run_mx(m, ts::MX_SWIGLU, m->tm_gu[l], L.wgu[l], 2 * F, d, M, h, L.mx, true, nullptr, act, nullptr, mx_out_of(m, d, F, M, L.mx2))
              : run_gemm_rows(m, ts::EPI_SWIGLU, m->tm_gu[l], m->tm_h, 2 * F, d, M, nullptr, act, nullptr, nullptr);
       if (s) return s;
-      s = mx ? run_mx(m, ts::MX_STORE, m->tm_d[l], L.wd[l], d, F, M, act, part, nullptr, nullptr)
+      s = mx ? run_mx(m, ts::MX_STORE, m->tm_d[l], L.wd[l], d, F, M, act, L.mx2, true, part, nullptr, nullptr, ts::MxOut{})
              : run_gemm_rows(m, ts::EPI_PARTIAL, m->tm_d[l], m->tm_act, d, F, M, part, nullptr, nullptr, &splits);
       if (s) return s;
     }
   }
   if (skip_head) return TS_OK;
   CU_TRY(ts::launch_add_norm(M, d, part, few ? 0 : splits, part_R, (const float *)m->W(L.gf), c.rms_eps, x, h, R, m->planes,
-                             m->st, m->stamp_slot()));
+                             mx_out_of(m, c.vocab, d, M, L.mx), m->st, m->stamp_slot()));
   m->launched(3);
   unsigned long long *amax = (unsigned long long *)m->WS(L.amax);
   ts_status s;
@@ -670,7 +685,7 @@ ts_status run_step(ts_model *m) {
     g.out = (float *)m->WS(L.logits); g.amax = amax;
     s = run_gemm_ws(m, ts::EPI_LOGITS, m->tm_lm, m->tm_h, c.vocab, d, M, g);
   } else if (mx) {
-    s = run_mx(m, ts::MX_LOGITS, m->tm_lm, L.lm_head, c.vocab, d, M, h, (float *)m->WS(L.logits), nullptr, amax);
+    s = run_mx(m, ts::MX_LOGITS, m->tm_lm, L.lm_head, c.vocab, d, M, h, L.mx, true, (float *)m->WS(L.logits), nullptr, amax, ts::MxOut{});
   } else {
     s = run_gemm_rows(m, ts::EPI_LOGITS, m->tm_lm, m->tm_h, c.vocab, d, M, (float *)m->WS(L.logits), nullptr, amax, nullptr);
   }

@@ -129,7 +129,7 @@ mx_quantise_kernel(const typename MxElem<TYPE>::raw *x, long long rows, int cols
       mx_widen8<TYPE>(raw[i], v);
       uint32_t top = 0;
       if constexpr (TYPE == MX_BF16) {   // (two at a time: their bits are the upper halves of fp32's)
-        const uint32_t *h = reinterpret_cast<const uint32_t *>(raw[i].r);
+        const uint32_t *h = raw[i].w;
         uint32_t m = __vmaxu2(__vmaxu2(h[0] & 0x7fff7fffu, h[1] & 0x7fff7fffu), __vmaxu2(h[2] & 0x7fff7fffu, h[3] & 0x7fff7fffu));
         top = max(m & 0xffff0000u, m << 16);
       } else {
@@ -218,24 +218,28 @@ mx_dequantise_kernel(const uint8_t *codes, const uint8_t *scales, long long rows
     for (int i = 0; i < kConvUnroll; ++i) {
       if (at[i] < 0) continue;
       const float f = scale_value(s[i]);
-      __align__(16) raw r[8];
+      uint32_t w[sizeof(raw) * 2];   // the eight elements, in words
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 t = from_e2m1x2(c[i] >> (8 * j));
-        r[2 * j] = mx_from_f32<TYPE>(t.x * f);
-        r[2 * j + 1] = mx_from_f32<TYPE>(t.y * f);
+        if constexpr (sizeof(raw) == 4) {
+          w[2 * j] = mx_from_f32<TYPE>(t.x * f);
+          w[2 * j + 1] = mx_from_f32<TYPE>(t.y * f);
+        } else {
+          w[j] = mx_from_f32<TYPE>(t.x * f) | (uint32_t)mx_from_f32<TYPE>(t.y * f) << 16;
+        }
       }
       if (left[i] >= 8) {
         if (sizeof(raw) == 4 && ((uintptr_t)d[i] & 31) == 0) {
-          st_global_v8(reinterpret_cast<float *>(d[i]), reinterpret_cast<const uint32_t *>(r));   // (whole sectors)
+          st_global_v8(reinterpret_cast<float *>(d[i]), w);   // (whole sectors)
         } else {
 #pragma unroll
-          for (int j = 0; j < (int)sizeof(raw) / 2; ++j) reinterpret_cast<uint4 *>(d[i])[j] = reinterpret_cast<const uint4 *>(r)[j];
+          for (int j = 0; j < (int)sizeof(raw) / 2; ++j) reinterpret_cast<uint4 *>(d[i])[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
         }
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (j < left[i]) d[i][j] = r[j];
+          if (j < left[i]) d[i][j] = (raw)(sizeof(raw) == 4 ? w[j] : w[j >> 1] >> (16 * (j & 1)));
       }
     }
   }

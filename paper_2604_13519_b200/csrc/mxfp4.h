@@ -46,7 +46,11 @@ struct MxArgs {
   __nv_bfloat16 *act_out;
   int act_rows, out_planes;
   unsigned long long *amax;
+  MxOut mo;                  // MX_SWIGLU: the output once more as planes
 };
+// bytes of 128 columns of the activations with `ncols` = planes x Mc instruction columns: elements, then scales
+__host__ __device__ inline int mx_x_block(int ncols) { return ncols * kMxTileK + 512 * ((ncols + 127) / 128); }
+
 enum : int { MX_STORE = 0, MX_SWIGLU = 1, MX_LOGITS = 2 };   // what a product does with its sums
 
 #ifdef __CUDACC__
@@ -67,78 +71,109 @@ template <int TYPE> __device__ __forceinline__ typename MxElem<TYPE>::raw mx_fro
 }
 
 // elements [c, c + 8) of a row of `cols` as they are, zeros behind its end and where `there` is false
-template <int TYPE> struct MxRaw8 { __align__(16) typename MxElem<TYPE>::raw r[TYPE == MX_PAIR ? 16 : 8]; };
+template <int TYPE> struct MxRaw8 { uint32_t w[TYPE == MX_F32 || TYPE == MX_PAIR ? 8 : 4]; };
 template <int TYPE>
 __device__ __forceinline__ void mx_fetch8(const typename MxElem<TYPE>::raw *p, long long pair, bool there, int c, int cols, bool vec, MxRaw8<TYPE> &x) {
   constexpr int kArrays = TYPE == MX_PAIR ? 2 : 1;
 #pragma unroll
   for (int h = 0; h < kArrays; ++h) {
-    const typename MxElem<TYPE>::raw *q = p + h * pair;
+    const typename MxElem<TYPE>::raw *q = p + h * pair + c;
+    uint32_t *w = x.w + 4 * h;
     if (vec && there && c + 8 <= cols) {
-      if (sizeof(x.r[0]) == 4 && ((uintptr_t)(q + c) & 31) == 0) {
-        ld_global_v8(q + c, reinterpret_cast<uint32_t *>(x.r));   // (whole sectors)
-        continue;
+      if constexpr (TYPE == MX_F32) {
+        if (((uintptr_t)q & 31) == 0) {
+          ld_global_v8(q, w);   // (whole sectors)
+          continue;
+        }
       }
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(x.r[0]) / 2; ++i) reinterpret_cast<uint4 *>(x.r + 8 * h)[i] = __ldg(reinterpret_cast<const uint4 *>(q + c) + i);
+      for (int i = 0; i < (TYPE == MX_F32 ? 2 : 1); ++i) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(q) + i);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x.r[8 * h + i] = there && c + i < cols ? q[c + i] : 0;
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t e = there && c + i < cols ? q[i] : 0u;
+        if constexpr (TYPE == MX_F32) w[i] = e;
+        else w[i >> 1] = i & 1 ? w[i >> 1] | e << 16 : e;
+      }
     }
   }
+}
+template <int TYPE> __device__ __forceinline__ float mx_elem(const MxRaw8<TYPE> &x, int i, int array) {
+  if constexpr (TYPE == MX_F32) return __uint_as_float(x.w[i]);
+  else return mx_to_f32<TYPE>((typename MxElem<TYPE>::raw)(x.w[4 * array + (i >> 1)] >> (16 * (i & 1))));
 }
 template <int TYPE> __device__ __forceinline__ void mx_widen8(const MxRaw8<TYPE> &x, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    v[i] = mx_to_f32<TYPE>(x.r[i]);
-    if constexpr (TYPE == MX_PAIR) v[i] += mx_to_f32<TYPE>(x.r[8 + i]);   // (exact: the second is the rounding remainder of the first)
+    v[i] = mx_elem<TYPE>(x, i, 0);
+    if constexpr (TYPE == MX_PAIR) v[i] += mx_elem<TYPE>(x, i, 1);   // (exact: the second is the rounding remainder of the first)
   }
 }
 
-// Eight elements at columns col .. col + 7 of row m (m: within its chunk) into the planes of a block of 128 columns (col: within it) at
-// `blk`; its scales lie `act_bytes` further on.  Four neighbouring threads share an MX block.
+// NE elements at columns col .. col + NE - 1 of row m (m: within its chunk) into the planes of a block of 128 columns (col: within it) at
+// `blk`; its scales lie `act_bytes` further on.  32 / NE neighbouring threads share an MX block.
 //
 // x as planes of e4m3 numbers (four significant bits each).  A block's first scale puts its largest magnitude into [2^7, 2^8), so that
 // it and what rounding leaves of it, at most 2^3, stay in range (448); the next plane holds sixteen times the remainder with a scale
 // of a sixteenth, and so on.  With two planes all bf16 numbers down to 2^-14 of the block's largest come out exactly (eight bits), and
 // what is lost of smaller ones is below 2^-21 of it; three planes do the same for fp16 (eleven bits).  Each remainder is exact in
 // fp32.  A block with an infinity or NaN gets the scale byte 255, which makes its products NaN.
-__device__ __forceinline__ void mx_to_planes(float (&v)[8], bool there, uint8_t *blk, int act_bytes, int Mc, int planes, int m, int col) {
+template <int NE>
+__device__ __forceinline__ void mx_to_planes(float (&v)[NE], bool there, uint8_t *blk, int act_bytes, int Mc, int planes, int m, int col) {
   uint32_t top = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  for (int j = 0; j < NE; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < 32 / NE; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
   if (!there) return;
   const uint32_t e = top >> 23;
   uint32_t s = e > 7u ? e - 7u : 0u;
   const float f = e == 255u ? 0.f : __uint_as_float((254u - s) << 23);   // 2^(127 - s)
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = e == 255u ? 0.f : v[j] * f;
+  for (int j = 0; j < NE; ++j) v[j] = e == 255u ? 0.f : v[j] * f;
   uint8_t *sc = blk + act_bytes + (col >> 5);
   for (int p = 0; p < planes; ++p) {
-    uint32_t q[2];
+    uint32_t q[(NE + 3) / 4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint16_t a, b;
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(a) : "f"(v[4 * h + 1]), "f"(v[4 * h]));
-      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(v[4 * h + 3]), "f"(v[4 * h + 2]));
-      q[h] = a | (uint32_t)b << 16;
-      uint32_t ha, hb;
-      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(ha) : "h"(a));
-      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(hb) : "h"(b));
-      const float2 fa = __half22float2(*reinterpret_cast<const __half2 *>(&ha)), fb = __half22float2(*reinterpret_cast<const __half2 *>(&hb));
-      v[4 * h] -= fa.x; v[4 * h + 1] -= fa.y; v[4 * h + 2] -= fb.x; v[4 * h + 3] -= fb.y;
+    for (int h = 0; h < NE / 2; ++h) {
+      uint16_t a;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(a) : "f"(v[2 * h + 1]), "f"(v[2 * h]));
+      q[h >> 1] = h & 1 ? q[h >> 1] | (uint32_t)a << 16 : a;
+      uint32_t back;
+      asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(a));
+      const float2 fa = __half22float2(*reinterpret_cast<const __half2 *>(&back));
+      v[2 * h] -= fa.x;
+      v[2 * h + 1] -= fa.y;
     }
     const int c = p * Mc + m;
-    *reinterpret_cast<uint2 *>(blk + c * kMxTileK + (((col >> 4) ^ (c & 7)) << 4) + (col & 8)) = make_uint2(q[0], q[1]);
-    if ((threadIdx.x & 3) == 0) sc[(c >> 7) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4] = (uint8_t)(e == 255u ? 255u : s);
+    uint8_t *d = blk + c * kMxTileK + (((col >> 4) ^ (c & 7)) << 4) + (col & 15);
+    if constexpr (NE == 8) *reinterpret_cast<uint2 *>(d) = make_uint2(q[0], q[1]);
+    else if constexpr (NE == 4) *reinterpret_cast<uint32_t *>(d) = q[0];
+    else *reinterpret_cast<uint16_t *>(d) = (uint16_t)q[0];
+    if ((col & 31) == 0) sc[(c >> 7) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4] = (uint8_t)(e == 255u ? 255u : s);
     const uint32_t next = s > 4u ? s - 4u : 0u;
     const float up = __uint_as_float((127u + s - next) << 23);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= up;
+    for (int j = 0; j < NE; ++j) v[j] *= up;
     s = next;
   }
+}
+
+// The same for a kernel that leaves its output as planes: row m and columns of the whole matrix, the elements as the bf16 planes beside
+// them have them.  By whole warps.
+template <int NE>
+__device__ __forceinline__ void mx_put(const MxOut &o, int m, int col, const __nv_bfloat16 (&hi)[NE], const __nv_bfloat16 (&lo)[NE], int bf16_planes) {
+  float v[NE];
+#pragma unroll
+  for (int j = 0; j < NE; ++j) v[j] = __bfloat162float(hi[j]) + (bf16_planes == 2 ? __bfloat162float(lo[j]) : 0.f);
+  const int z = m / o.Mc, ncols = o.planes * o.Mc;
+  mx_to_planes<NE>(v, true, o.out + ((size_t)z * o.n_kb + (col >> 7)) * mx_x_block(ncols), ncols * kMxTileK, o.Mc, o.planes, m - z * o.Mc, col & 127);
+}
+__device__ __forceinline__ void mx_clear_flags(const MxOut &o, int thread, int threads) {
+  for (int i = thread; i < o.n_flags; i += threads) o.flags[i] = 0;
 }
 
 // What becomes of four finished sums: row mg, features n .. n + 3 (a warp's lanes hold 128 consecutive ones)
@@ -185,6 +220,10 @@ template <int EPI> __device__ __forceinline__ void mx_finish(const MxArgs &g, lo
             *reinterpret_cast<__nv_bfloat162 *>(g.act_out + (size_t)mg * F + f) = __halves2bfloat162(h0, h1);
             if (g.out_planes == 2)
               *reinterpret_cast<__nv_bfloat162 *>(g.act_out + ((size_t)g.act_rows + mg) * F + f) = __halves2bfloat162(l0, l1);
+            if (g.mo.out) {
+              const __nv_bfloat16 hi[2] = {h0, h1}, lo[2] = {l0, l1};
+              mx_put<2>(g.mo, (int)mg, f, hi, lo, g.out_planes);
+            }
           }
 }
 #endif
@@ -216,8 +255,8 @@ cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const Mx
                               bool pdl, int *launches);
 // early: as in MxArgs; else the product is let start when all that came before this kernel is done.
 cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, bool early, cudaStream_t st, bool pdl);
-// bytes of 128 columns of the activations with `ncols` = planes x Mc instruction columns: elements, then scales
-__host__ __device__ inline int mx_x_block(int ncols) { return ncols * kMxTileK + 512 * ((ncols + 127) / 128); }
+// ... or what makes the input leaves it there.
+MxOut mx_out(int n_kb, int planes, void *scratch, const MxPlan &p);
 
 cudaError_t launch_mx_quantise(const void *x, int type, int rows, int cols, long long ldx, uint8_t *codes, uint8_t *scales, cudaStream_t st);
 cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, int rows, int cols, void *y, int type, long long ldy,

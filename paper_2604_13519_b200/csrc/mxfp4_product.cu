@@ -313,6 +313,7 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
     const int f = q * 32 + lane;                  // this thread's feature of a tile
     const uint32_t stg = smem_u32(staging);
     pdl_wait();   // (flags are cleared by the kernel before; outputs may still be read by its consumers)
+    if (EPI == MX_SWIGLU && cta == 0 && warp == 2) mx_clear_flags(g.mo, lane, 32);
     int j = 0, turn = 0;
     bool alive = true;   // (all warps go through the same barriers whatever becomes of a wait; after one has expired none is waited for)
     for (long long hi = u1; hi > u0; ++j) {
@@ -390,6 +391,10 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tmap_w, const MxArgs g) {
     // The sums go through the ring's shared memory (free by now: every copy was consumed by a product that has completed) to
     // [row][128 features]; then a warp takes every fourth row with four consecutive features per lane.  The rows are dealt out over the
     // CTAs of a cluster, which add the slices' sums in slice order.
+    if (EPI == MX_SWIGLU && cta == 0 && split == 0 && warp == 2) {
+      pdl_wait();
+      mx_clear_flags(g.mo, lane, 32);
+    }
     const int q = warp & 3, item = cta, tile = item / g.chunks, m0 = (item - tile * g.chunks) * g.Mc, M = min(g.Mc, g.M - m0);
     pdl_wait();   // outputs of this kernel may still be read by the previous one's consumers
     const bool done = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_full[0]), 0));
@@ -600,6 +605,12 @@ static cudaError_t prod_launch(const CUtensorMap &tw, const MxArgs &g, const MxP
     case MX_PAIR: return prod_launch_own<EPI, MX_PAIR>(tw, g, p, smem, st, pdl);
     default: return prod_launch_own<EPI, MX_F32>(tw, g, p, smem, st, pdl);
   }
+}
+
+MxOut mx_out(int n_kb, int planes, void *scratch, const MxPlan &p) {
+  if (p.own) return MxOut{};
+  const MxScratch w = mx_scratch(n_kb, planes, p);
+  return MxOut{(uint8_t *)scratch, p.Mc, planes, n_kb, (int *)((uint8_t *)scratch + w.flags), p.stream ? (p.apart ? p.chunks : 1) * p.ctas : 0};
 }
 
 cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const MxInput &in, void *scratch, const MxPlan &p, cudaStream_t st,
