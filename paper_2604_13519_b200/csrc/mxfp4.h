@@ -11,8 +11,9 @@ constexpr int kMxTileN = 128;         // weight rows of a stored block
 constexpr int kMxCodeBytes = kMxTileN * kMxTileK / 2;
 constexpr int kMxTileBytes = kMxCodeBytes + kMxTileN * (kMxTileK / kMxBlock);   // codes, then scales: 8704
 
-// A laid-out matrix of N x K: ceil(N / 128) x ceil(K / 128) blocks, a tile's blocks one after the other.  Inside a block: elements [128 rows][64 bytes], the even one of two in the low half of a byte, then scales [32][4][4]: bytes of row 32 j + l at
-// [l][j], one per MX block (the order in which tcgen05.cp takes them to tensor memory).
+// A laid-out matrix of N x K: ceil(N / 128) x ceil(K / 128) blocks, a tile's blocks one after the other.  Inside a block: elements
+// [128 rows][64 bytes], the even one of two in the low half of a byte, then scales [32][4][4]: bytes of row 32 j + l at [l][j], one per
+// MX block (the order in which tcgen05.cp takes them to tensor memory).
 __host__ __device__ inline int mx_scale_at(int row) { return kMxCodeBytes + (row & 31) * 16 + (row >> 5) * 4; }
 
 __host__ __device__ inline int mx_block(int tile, int kb, int n_kb) { return tile * n_kb + kb; }
@@ -23,7 +24,7 @@ inline int mx_planes_of(int type) { return type == MX_BF16 ? 2 : type == MX_F16 
 
 struct MxArgs {
   const uint8_t *w;          // laid-out matrix
-  const void *x;             // the activations' planes, see launch_mx_planes8; with plan.own the rows themselves:
+  const void *x;             // the activations' planes, see launch_mx_input; with plan.own the rows themselves:
   long long ldx, pair;       // row stride; MX_PAIR: distance of the two arrays, in elements
   int x_type, vec_x, K;      // type, rows can be read 16 bytes at a time, columns
   float *slabs;              // [CTA][Mc][128] sums of tiles that the CTA has without their last k-blocks
@@ -178,53 +179,53 @@ __device__ __forceinline__ void mx_clear_flags(const MxOut &o, int thread, int t
 
 // What becomes of four finished sums: row mg, features n .. n + 3 (a warp's lanes hold 128 consecutive ones)
 template <int EPI> __device__ __forceinline__ void mx_finish(const MxArgs &g, long long mg, int n, const float (&v)[4], int lane) {
-          if constexpr (EPI == MX_STORE) {
-            if (g.y_type == MX_F32) {
-              float *d = (float *)g.y + mg * g.ldy + n;
-              if (g.vec && n + 4 <= g.N) {
-                *reinterpret_cast<float4 *>(d) = make_float4(v[0], v[1], v[2], v[3]);
-              } else {
-                for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = v[j];
-              }
-            } else {
-              uint16_t h[4];
-              for (int j = 0; j < 4; ++j)
-                h[j] = g.y_type == MX_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v[j])) : __half_as_ushort(__float2half_rn(v[j]));
-              uint16_t *d = (uint16_t *)g.y + mg * g.ldy + n;
-              if (g.vec && n + 4 <= g.N) {
-                *reinterpret_cast<uint2 *>(d) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-              } else {
-                for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = h[j];
-              }
-            }
-          } else if constexpr (EPI == MX_LOGITS) {
-            *reinterpret_cast<float4 *>(g.out + (size_t)mg * g.N + n) = make_float4(v[0], v[1], v[2], v[3]);
-            // order-preserving map of the float to an unsigned word; ties resolve to the lowest id (lowest lane, then
-            // lowest of its four)
-            uint32_t best = 0;
-            int bi = 0;
-  #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint32_t u = __float_as_uint(v[j]);
-              u = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-              if (u > best) { best = u; bi = j; }
-            }
-            const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-            if (lane == __ffs(__ballot_sync(0xffffffffu, best == top)) - 1)
-              atomicMax(g.amax + (size_t)mg * kAmaxStride, ((unsigned long long)top << 32) | (unsigned long long)(0xFFFFFFFFu - (uint32_t)(n + bi)));
-          } else {  // MX_SWIGLU: even feature row = gate_f, odd = up_f, f = n / 2
-            __nv_bfloat16 h0, l0, h1, l1;
-            split_bf16(v[0] / (1.f + __expf(-v[0])) * v[1], h0, l0);
-            split_bf16(v[2] / (1.f + __expf(-v[2])) * v[3], h1, l1);
-            const int F = g.N >> 1, f = n >> 1;
-            *reinterpret_cast<__nv_bfloat162 *>(g.act_out + (size_t)mg * F + f) = __halves2bfloat162(h0, h1);
-            if (g.out_planes == 2)
-              *reinterpret_cast<__nv_bfloat162 *>(g.act_out + ((size_t)g.act_rows + mg) * F + f) = __halves2bfloat162(l0, l1);
-            if (g.mo.out) {
-              const __nv_bfloat16 hi[2] = {h0, h1}, lo[2] = {l0, l1};
-              mx_put<2>(g.mo, (int)mg, f, hi, lo, g.out_planes);
-            }
-          }
+  if constexpr (EPI == MX_STORE) {
+    if (g.y_type == MX_F32) {
+      float *d = (float *)g.y + mg * g.ldy + n;
+      if (g.vec && n + 4 <= g.N) {
+        *reinterpret_cast<float4 *>(d) = make_float4(v[0], v[1], v[2], v[3]);
+      } else {
+        for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = v[j];
+      }
+    } else {
+      uint16_t h[4];
+      for (int j = 0; j < 4; ++j)
+        h[j] = g.y_type == MX_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v[j])) : __half_as_ushort(__float2half_rn(v[j]));
+      uint16_t *d = (uint16_t *)g.y + mg * g.ldy + n;
+      if (g.vec && n + 4 <= g.N) {
+        *reinterpret_cast<uint2 *>(d) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+      } else {
+        for (int j = 0; j < 4; ++j) if (n + j < g.N) d[j] = h[j];
+      }
+    }
+  } else if constexpr (EPI == MX_LOGITS) {
+    *reinterpret_cast<float4 *>(g.out + (size_t)mg * g.N + n) = make_float4(v[0], v[1], v[2], v[3]);
+    // order-preserving map of the float to an unsigned word; ties resolve to the lowest id (lowest lane, then
+    // lowest of its four)
+    uint32_t best = 0;
+    int bi = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t u = __float_as_uint(v[j]);
+      u = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+      if (u > best) { best = u; bi = j; }
+    }
+    const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+    if (lane == __ffs(__ballot_sync(0xffffffffu, best == top)) - 1)
+      atomicMax(g.amax + (size_t)mg * kAmaxStride, ((unsigned long long)top << 32) | (unsigned long long)(0xFFFFFFFFu - (uint32_t)(n + bi)));
+  } else {  // MX_SWIGLU: even feature row = gate_f, odd = up_f, f = n / 2
+    __nv_bfloat16 h0, l0, h1, l1;
+    split_bf16(v[0] / (1.f + __expf(-v[0])) * v[1], h0, l0);
+    split_bf16(v[2] / (1.f + __expf(-v[2])) * v[3], h1, l1);
+    const int F = g.N >> 1, f = n >> 1;
+    *reinterpret_cast<__nv_bfloat162 *>(g.act_out + (size_t)mg * F + f) = __halves2bfloat162(h0, h1);
+    if (g.out_planes == 2)
+      *reinterpret_cast<__nv_bfloat162 *>(g.act_out + ((size_t)g.act_rows + mg) * F + f) = __halves2bfloat162(l0, l1);
+    if (g.mo.out) {
+      const __nv_bfloat16 hi[2] = {h0, h1}, lo[2] = {l0, l1};
+      mx_put<2>(g.mo, (int)mg, f, hi, lo, g.out_planes);
+    }
+  }
 }
 #endif
 

@@ -24,7 +24,7 @@
 // distributed shared memory: less of an exchange than through L2, which counts where a CTA has few k-blocks.
 //
 // Up to two or four rows the CTAs of the second kind make the planes themselves (kOwn): four more warps turn a stage's 128 columns into e4m3
-// on the way into shared memory, which saves a launch; for more rows a kernel ahead does it once for all CTAs (launch_mx_planes8).
+// on the way into shared memory, which saves a launch; for more rows a kernel ahead does it once for all CTAs (launch_mx_input).
 //
 // Roles: warp 0 = copies, warp 1 = tensor memory, scales and products, warps 2..5 = epilogue, warps 6.. = planes (kOwn).
 // Every wait is bounded; on expiry the CTA records an error word and leaves through the normal exit.
@@ -508,7 +508,7 @@ static size_t prod_stage_bytes(int planes, int Mc) {
 // memory (weights 16 KB, columns x 128, all of it written and read, 128 a cycle).  301 rows of fp16 x 4096 x 12288, 160 tiles: 66 -> 63 us;
 // 64 rows x 24576 x 4096, 192 tiles: 21 us and 28 in runs, 112 rows 31 and 39.
 // Rows whose planes the product makes itself: up to two, and up to four where a CTA has few blocks (its warps make a block of four rows in
-// about as long as a block of two takes to be multiplied; 4096 x 4096 at 4 rows 8.4 -> 7.4 us, 24576 x 4096 at 3 rows 15.4 and 17.1).
+// about as long as a block of two takes to be multiplied; 4096 x 4096 at 4 rows 8.4 -> 6.5 us, 24576 x 4096 at 3 rows 15.4 and 17.1).
 constexpr int kOwnRows = 2, kOwnRowsShort = 4, kOwnShort = 8;
 constexpr int kRunCycles = 25000;
 MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits) {
