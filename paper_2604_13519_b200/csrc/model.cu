@@ -353,7 +353,7 @@ ts_status make_map(EncodeTiledFn enc, CUtensorMap *out, void *base, int rank, co
 // of DRAM pages.
 ts_status weight_map(EncodeTiledFn enc, const ts_model_config &c, CUtensorMap *out, void *base, uint64_t N, uint64_t K) {
   if (c.weights == TS_WEIGHTS_MXFP4) {
-    const int r = ts::mx_weight_map((void *)enc, out, base, N / ts::kMxTileN * ((K + ts::kMxTileK - 1) / ts::kMxTileK));
+    const int r = ts::mx_weight_map(out, base, N / ts::kMxTileN * ((K + ts::kMxTileK - 1) / ts::kMxTileK));
     return r ? fail(TS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", r) : TS_OK;
   }
   const uint64_t dims[2] = {64, N * (K / 64)};

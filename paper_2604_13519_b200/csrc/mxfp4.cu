@@ -386,12 +386,33 @@ cudaError_t launch_mx_input(const MxInput &in, void *scratch, const MxPlan &p, b
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-int mx_weight_map(void *encode, CUtensorMap *map, const void *data, uint64_t blocks) {
+static std::atomic<EncodeTiledFn> g_encode{nullptr};
+static EncodeTiledFn encode_fn() {
+  EncodeTiledFn fn = g_encode.load(std::memory_order_acquire);
+  if (!fn) {   // (two threads that come here at once find the same)
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+    fn = (EncodeTiledFn)p;
+    g_encode.store(fn, std::memory_order_release);
+  }
+  return fn;
+}
+int mx_weight_map(CUtensorMap *map, const void *data, uint64_t blocks) {
+  const EncodeTiledFn encode = encode_fn();
+  if (!encode) return CUDA_ERROR_NOT_FOUND;
   const cuuint64_t dims[3] = {kMxTileK, kMxTileN, blocks}, strides[2] = {kMxTileK / 2, kMxTileBytes};
   const cuuint32_t box[3] = {kMxTileK, kMxTileN, 1}, es[3] = {1, 1, 1};
-  return (int)((EncodeTiledFn)encode)(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 3, const_cast<void *>(data), dims, strides, box, es,
-                                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-                                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 3, const_cast<void *>(data), dims, strides, box, es,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+int mx_rows_map(CUtensorMap *map, const void *data, uint64_t rows, int box_rows) {
+  const EncodeTiledFn encode = encode_fn();
+  if (!encode) return CUDA_ERROR_NOT_FOUND;
+  const cuuint64_t dims[2] = {128, rows}, strides[1] = {128};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, es[2] = {1, 1};
+  return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(data), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
 }  // namespace ts
@@ -403,8 +424,6 @@ using ts::set_error;
 
 constexpr int64_t kMostSide = 1 << 21;   // rows and columns of a matrix
 
-using ts::EncodeTiledFn;
-
 // What a device offers, asked for once per device.
 struct MxDevice {
   int sms = 0;
@@ -413,7 +432,6 @@ struct MxDevice {
 constexpr int kMaxDevices = 64;
 MxDevice g_dev[kMaxDevices];
 std::atomic<uint64_t> g_dev_known{0};
-std::atomic<EncodeTiledFn> g_encode{nullptr};
 
 ts_status device_of_call(MxDevice *out) {
   int dev = 0;
@@ -426,13 +444,6 @@ ts_status device_of_call(MxDevice *out) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return set_error(TS_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(e));
     if (major != 10) return set_error(TS_ERR_CUDA, "device is not an sm_100 part; this library is built for sm_100a only");
-    if (!g_encode.load(std::memory_order_acquire)) {
-      void *fn = nullptr;
-      cudaDriverEntryPointQueryResult q;
-      e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
-      if (e != cudaSuccess || !fn || q != cudaDriverEntryPointSuccess) return set_error(TS_ERR_CUDA, "cuTensorMapEncodeTiled not available");
-      g_encode.store((EncodeTiledFn)fn, std::memory_order_release);
-    }
     g_dev[dev].sms = sms;   // (two threads that come here at once store the same)
     ts::mx_fits(g_dev[dev].fits);
     g_dev_known.fetch_or(1ull << dev, std::memory_order_release);
@@ -532,7 +543,7 @@ ts_status ts_mxfp4_matrix_init(ts_mxfp4_matrix *m, const void *data, int64_t n, 
   MX_OK(device_of_call(&d));
   CUtensorMap map;
   static_assert(sizeof map == sizeof m->map, "a descriptor has 128 bytes");
-  const CUresult r = (CUresult)ts::mx_weight_map((void *)g_encode.load(std::memory_order_acquire), &map, data, tiles_of(n) * kblocks_of(k));
+  const CUresult r = (CUresult)ts::mx_weight_map(&map, data, tiles_of(n) * kblocks_of(k));
   if (r != CUDA_SUCCESS) return set_error(TS_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
   m->data = data;
   std::memcpy(m->map, &map, sizeof map);

@@ -366,3 +366,31 @@ def test_few_rows_many_times(x_type):
             for _ in range(20):
                 assert torch.equal(ts.ts_mxfp4_product(w, x[:m], torch.float32), whole[:m]), (n, k, m)
         w.check()
+
+
+@pytest.mark.parametrize("m,n,k", [(33, 39000, 2100), (80, 77900, 2100), (113, 39000, 2100), (225, 2049, 1000), (700, 10100, 2100), (1500, 4900, 2111),
+                                   (8200, 1030, 2100), (1000, 41000, 300)])
+@pytest.mark.parametrize("x_type", TYPES)
+def test_many_rows(m, n, k, x_type):
+    """Rows in one and several chunks, odd numbers of tiles, runs that begin and end anywhere; twice on the same memory, once captured."""
+    rng = np.random.default_rng(m + n + k)
+    codes, scales, w = _weights(rng, n, k)
+    _, x = _strided(rng.standard_normal((m, k)), TYPES[x_type], k + 5)
+    held = torch.full((m + 2, n + 3), 9., device="cuda")
+    y = held[1:m + 1, :n]
+    ws = w.workspace(m, TYPES[x_type])
+    ts.ts_mxfp4_product(w, x, out=y, workspace=ws)
+    w.check()
+    _check(y, x, ref.values(codes, scales, k), k, torch.float32)
+    first = y.clone()
+    ws.fill_(255)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ts.ts_mxfp4_product(w, x, out=y, workspace=ws)
+    for _ in range(3):
+        y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, first)
+    w.check()
+    assert (held[0] == 9).all() and (held[-1] == 9).all() and (held[:, n:] == 9).all()
