@@ -281,6 +281,7 @@ struct ts_model {
   float last_inv_t = 1.f;                      // 1 / temperature of that step
   size_t smem_optin = 0;
   int max_clusters[9] = {};                    // [c] = clusters of c CTAs of the weight-streaming kernel that fit at once
+  int mx_fits[9] = {};                         // (see mx_plan)
   // per-kernel timing pass (ts_profile_step): one event after every launch
   bool profiling = false;
   std::vector<cudaEvent_t> prof_ev;
@@ -445,7 +446,7 @@ ts_status run_gemm_ws(ts_model *m, int epi, const CUtensorMap &tw, const CUtenso
 // `down` apart from the others, since gate-up reads its own while it writes that).
 ts::MxPlan mx_plan_of(const ts_model *m, int N, int K, int M) {
   return ts::mx_plan(M, N / ts::kMxTileN, (K + ts::kMxTileK - 1) / ts::kMxTileK, m->planes == 2 ? ts::mx_planes_of(ts::MX_PAIR) : ts::mx_planes_of(ts::MX_BF16),
-                     m->n_sms, m->max_clusters);
+                     m->n_sms, m->mx_fits, false);
 }
 ts::MxOut mx_out_of(const ts_model *m, int N, int K, int M, uint64_t scratch) {
   if (m->c.weights != TS_WEIGHTS_MXFP4 || K % ts::kMxTileK) return ts::MxOut{};   // (a last block with nothing in its second half: launch_mx_input fills it)
@@ -1270,6 +1271,7 @@ ts_status ts_init_model(const ts_model_config *cfg, const ts_buffers *bufs, void
     cudaDeviceGetAttribute(&optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
     m->smem_optin = (size_t)optin;
     for (int cl = 1; cl <= 8; ++cl) m->max_clusters[cl] = ts::gemm_max_clusters(cl, m->gemm_smem_budget);
+    ts::mx_fits(m->mx_fits);
     m->fused_ok = coop != 0 && m->n_sms <= kMaxFusedCtas &&
                   ts::fused_ring_stages(m->planes, kFusedMaxRows, c.head_dim, m->smem_optin) >= 2;
   }

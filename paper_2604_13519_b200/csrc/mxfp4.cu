@@ -589,7 +589,7 @@ ts_status ts_mxfp4_product(const ts_mxfp4_product_args *a, void *stream) {
   g.vec = a->ldy % 4 == 0 && (uintptr_t)a->y % (4 * ysz) == 0;
   const ts::MxInput in{a->x, a->x_type, (int)M, (int)K, a->ldx, 0};
   const int planes = ts::mx_planes_of(a->x_type);
-  const ts::MxPlan p = ts::mx_plan((int)M, g.tiles, g.n_kb, planes, d.sms, d.fits);
+  const ts::MxPlan p = ts::mx_plan((int)M, g.tiles, g.n_kb, planes, d.sms, d.fits, true);
   const uint64_t need = ts::mx_scratch(g.n_kb, planes, p).bytes;
   if (need && (!a->workspace || a->workspace_bytes < need || (uintptr_t)a->workspace % 128))
     return set_error(TS_ERR_ARG, "workspace of %llu bytes, 128-byte aligned, needed for these rows", (unsigned long long)need);

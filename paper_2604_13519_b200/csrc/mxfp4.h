@@ -233,8 +233,9 @@ template <int EPI> __device__ __forceinline__ void mx_finish(const MxArgs &g, lo
 // How a product is dealt out: activation rows per chunk (a multiple of 8, planes x rows one of 16), chunks; runs of k-blocks
 // (stream; apart: a launch per chunk; pairs: to pairs of CTAs) or a tile to each of `ctas` clusters; whether it makes the planes itself.
 struct MxPlan { int Mc, chunks, ctas, cluster; bool stream, apart, own, pairs; };
-// fits[c]: clusters of c CTAs that the device runs at once, two CTAs to an SM, fits[0]: pairs of one to an SM (mx_fits); null: none are made.
-MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits);
+// fits[c]: clusters of c CTAs that the device runs at once, two CTAs to an SM, fits[0]: pairs of one to an SM (mx_fits); null: none are made.  alone: no kernel
+// before the product could leave the planes.
+MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits, bool alone);
 void mx_fits(int (&fits)[9]);
 
 // Activations, and the scratch memory of a product with them: planes, and for products dealt out in runs flags and slabs.

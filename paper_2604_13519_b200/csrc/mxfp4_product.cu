@@ -363,7 +363,7 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
     bool ok = true;
     int s = 0, j = 0;
     uint32_t ph = 0;
-    int set = 0, ahead = 0, done = 0;    // columns for scales; where there are fewer than stages: blocks issued since stage `done` was filled
+    int set = 0, ahead = 0, done = 0;    // (pairs) columns for scales; where there are fewer than stages: blocks issued since stage `done` was filled
     uint32_t done_ph = 0;
     for (long long hi = u1; ok && hi > u0; ++j) {
       const ProdSeg t = prod_seg(g, u0, hi);
@@ -381,7 +381,7 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
         const int s1 = wrap ? 0 : s + 1;
         const uint32_t ph1 = wrap ? ph ^ 1 : ph;
         ok = __all_sync(0xffffffffu, prod_wait<kPair>(smem_u32(&ctl->full[s]), ph) && (!pair || prod_wait<kPair>(smem_u32(&ctl->full[s1]), ph1)));
-        if (g.sets < g.stages) {   // the products that read the columns to be written are done
+        if (kPair && g.sets < g.stages) {   // the products that read the columns to be written are done
           for (ahead += 1 + pair; ok && ahead > g.sets; --ahead) {
             ok = __all_sync(0xffffffffu, prod_wait<kPair>(smem_u32(&ctl->empty[done]), done_ph));
             if (++done == g.stages) { done = 0; done_ph ^= 1; }
@@ -392,10 +392,10 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
           break;
         }
         tc_fence_after();
-        const int set1 = set + 1 == g.sets ? 0 : set + 1;
+        const int set0 = kPair ? set : s, set1 = !kPair ? s1 : set + 1 == g.sets ? 0 : set + 1;
         const uint32_t a0 = smem_u32(smem) + s * stage_bytes, a1 = smem_u32(smem) + s1 * stage_bytes;
         if (elect_one()) {
-          prod_block<kPair>(a0, scales + set * set_cols, d, idesc, act_bytes, sb_words, kb != t.kb0);
+          prod_block<kPair>(a0, scales + set0 * set_cols, d, idesc, act_bytes, sb_words, kb != t.kb0);
           prod_commit<kPair>(smem_u32(&ctl->empty[s]));
           if (pair) {
             prod_block<kPair>(a1, scales + set1 * set_cols, d, idesc, act_bytes, sb_words, true);
@@ -409,7 +409,7 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
           ph = ph1;
           set = set1;
         }
-        if (++set == g.sets) set = 0;
+        if (kPair && ++set == g.sets) set = 0;
         if (++s == g.stages) { s = 0; ph ^= 1; }
       }
       if (elect_one()) {
@@ -441,16 +441,15 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
       const int M = tile < g.tiles ? min(g.Mc, g.M - m0) : 0;
       const bool finish = t.kb1 == g.n_kb;   // else another CTA finishes the tile
       int before = cta;                      // CTAs [before, cta) have its earlier k-blocks
-      bool there = alive;
+      bool there = true;                     // their partial sums are
       if (finish && M > 0 && t.kb0 > 0) {
         const long long first = (long long)t.item * g.n_kb;
         do --before;
         while (prod_start(g, before, G) > first);
-        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, wait_flag(g.flags + kCtas * c + rank));
-        if (alive && !there && lane == 0) prod_error(g, DEV_TIMEOUT_GRID);
+        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, ld_acquire(g.flags + kCtas * c + rank));
       }
-      // The CTAs' partial sums, 32 rows ahead of use: the first of them are under way while the tile's last products run.  (Eight rows ahead, and
-      // from there on, a run's end took 12 us longer where it had partial sums to fetch.)
+      // The CTAs' partial sums, 32 rows ahead of use: the first of them are under way while the tile's last products run, unless they are late (as
+      // they are where a run is shorter than a tile).  With eight rows ahead the end of a pair's run took 12 us longer where it had any to fetch.
       float part[4][8];
       auto fetch = [&](int c0, float (&p)[8]) {
 #pragma unroll
@@ -466,11 +465,20 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
           }
         }
       };
+      if (there) {
 #pragma unroll
-      for (int h = 0; h < 4; ++h) fetch(mine + 8 * h, part[h]);
+        for (int h = 0; h < 4; ++h) fetch(mine + 8 * h, part[h]);
+      }
       bool ok = alive && __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_full[b]), use & 1));
       if (alive && !ok && lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
       alive = ok;
+      if (!there) {
+        there = ok;
+        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, wait_flag(g.flags + kCtas * c + rank));
+        if (ok && !there && lane == 0) prod_error(g, DEV_TIMEOUT_GRID);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) fetch(mine + 8 * h, part[h]);
+      }
       tc_fence_after();
       ok = ok && there && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
       const uint32_t taddr = tmem_base + b * acc_cols + ((uint32_t)(q * 32) << 16);
@@ -647,12 +655,14 @@ static size_t prod_stage_bytes(int planes, int Mc, bool pairs) {
 // own.
 //
 // Runs where there are more tiles than places, and where tiles do not come out even over the SMs and the time that costs is worth the
-// second exchange at a run's end, 7 to 12 us.  An SM takes a block in about 256 + 2 x columns cycles, the time of its bytes through shared
-// memory (weights 16 KB, columns x 128, all of it written and read, 128 a cycle).  301 rows of fp16 x 4096 x 12288, 160 tiles: 66 -> 63 us;
-// 64 rows x 24576 x 4096, 192 tiles: 21 us and 28 in runs, 112 rows 31 and 39.
+// second exchange at a run's end, 7 to 12 us: 64 rows x 20480 x 12288, 160 tiles, 51 -> 46 us; 64 rows x 24576 x 4096, 192 tiles, 21
+// and 28.  (An SM takes a block in about 256 + 2 x columns cycles, the time of its bytes through shared memory: weights 16 KB, columns x 128, all of it
+// written and read, 128 a cycle.  The rule counts 32 columns: with 224, 112 rows x 20480 x 8192 took 56 us in runs and 54 in tiles.)
 // Rows whose planes the product makes itself: up to two, and up to four where a CTA has few blocks (its warps make a block of four rows in
 // about as long as a block of two takes to be multiplied; 4096 x 4096 at 4 rows 8.4 -> 6.5 us, 24576 x 4096 at 3 rows 15.4 and 17.1).
-constexpr int kOwnRows = 2, kOwnRowsShort = 4, kOwnShort = 8;
+// Up to eight bf16 rows take as long that way as with a launch for the planes (2048 x 8192 at 8 rows 9.0 and 8.9 us; fp16 9.5 and 8.8, fp32 11.5
+// and 8.8), but cost a call of its own one launch less on the host (12.3 -> 9.5 us).
+constexpr int kOwnRows = 2, kOwnRowsShort = 4, kOwnRowsAlone = 8, kOwnShort = 8;
 constexpr int kRunCycles = 25000;
 // Equal chunks of at most `cols` instruction columns (planes x rows), of which there are a multiple of 16, with pairs of CTAs of 32.
 static int mx_step(int planes, bool pairs) { return pairs ? (planes % 4 == 0 ? 8 : planes % 2 == 0 ? 16 : 32) : planes % 2 ? 16 : 8; }
@@ -677,7 +687,7 @@ static MxPlan mx_cut_pairs(int M, int planes) {
 // they save: 1024 rows x 4096 x 4096 (76 blocks) 55 -> 43 us, 128 x 24576 x 4096 (83) 44 -> 37, 512 x 6144 x 4096 (62) 33 and 37, 1024 x 24576 x 4096
 // 197 -> 187, 96 x 151936 x 4096 140 -> 102, 1000 x 4096 x 4096 of fp32 98 -> 79.
 constexpr int kPairBlocks = 70;
-MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits) {
+MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits, bool alone) {
   MxPlan p = mx_cut(M, planes, false, kProdAcc);
   n_sms = std::min(n_sms, kMxMostSms);
   const bool same = M <= (planes == 5 ? 32 : 64);
@@ -692,7 +702,7 @@ MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fit
     }
   }
   const long long items = (long long)tiles * (same ? 1 : p.chunks), places = (long long)kProdCtas * n_sms;
-  const long long uneven = ((items + n_sms - 1) / n_sms * n_sms - items) * n_kb * (256 + 2 * (same ? 32 : planes * p.Mc)) / n_sms;
+  const long long uneven = ((items + n_sms - 1) / n_sms * n_sms - items) * n_kb * (256 + 2 * 32) / n_sms;
   p.apart = same && p.chunks > 1;
   p.stream = items > n_sms && items * n_kb >= 4 * places && ((items > places && (same || p.chunks == 1)) || uneven > kRunCycles);
   // (A tenth more than are needed must fit: how many do depends on how the device's SMs are grouped, and one that finds its place taken runs
@@ -701,7 +711,7 @@ MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fit
   for (int c = 2; fits && !p.stream && c <= 8 && c <= n_kb; ++c)
     if (fits[c] * 10ll >= items * 11) p.cluster = c;
   p.ctas = (int)(p.stream ? places : (long long)tiles * p.chunks);
-  p.own = !p.stream && M <= (n_kb <= kOwnShort * p.cluster ? kOwnRowsShort : kOwnRows);
+  p.own = !p.stream && M <= (n_kb > kOwnShort * p.cluster ? kOwnRows : alone && planes == 2 ? kOwnRowsAlone : kOwnRowsShort);
   return p;
 }
 
@@ -774,7 +784,10 @@ static cudaError_t prod_launch_one(const ProdMaps<true> &maps, const MxArgs &g, 
 
 template <int EPI, int TYPE>
 static cudaError_t prod_launch_own(const ProdMaps<true> &maps, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
-  return g.M <= 2 ? prod_launch_one<EPI, kTile, 1, TYPE>(maps, g, p, smem, st, pdl) : prod_launch_one<EPI, kTile, 2, TYPE>(maps, g, p, smem, st, pdl);
+  if (g.M <= 2) return prod_launch_one<EPI, kTile, 1, TYPE>(maps, g, p, smem, st, pdl);
+  if (g.M <= 4) return prod_launch_one<EPI, kTile, 2, TYPE>(maps, g, p, smem, st, pdl);
+  if constexpr (EPI == MX_STORE && TYPE == MX_BF16) return prod_launch_one<EPI, kTile, 4, TYPE>(maps, g, p, smem, st, pdl);
+  return cudaErrorInvalidValue;
 }
 template <int EPI>
 static cudaError_t prod_launch(const ProdMaps<true> &maps, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {

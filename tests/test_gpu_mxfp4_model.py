@@ -74,7 +74,7 @@ def test_steps_against_the_oracle(name, ctx, ks, act_split):
             assert err.max() <= 0.15 and err.mean() <= 0.02, (k, err.max(), err.mean())
 
 
-@pytest.mark.parametrize("name,rows", [("tiny", (64, 40, 1)), ("odd", (64, 33, 50)), ("1b-2l", (50, 64, 30))])
+@pytest.mark.parametrize("name,rows", [("tiny", (64, 40, 1)), ("odd", (64, 33, 50)), ("1b-2l", (50, 64, 30)), ("8b-2l", (40, 30))])
 def test_batches_against_the_oracle(name, rows):
     shape = SHAPES[name]
     om = oracle.OracleModel(shape, _weights(name)[1])
