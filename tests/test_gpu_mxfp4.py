@@ -394,3 +394,25 @@ def test_many_rows(m, n, k, x_type):
         assert torch.equal(y, first)
     w.check()
     assert (held[0] == 9).all() and (held[-1] == 9).all() and (held[:, n:] == 9).all()
+
+
+def test_many_rows_on_two_streams_beside_few():
+    """Products by pairs of CTAs on two streams, on a third one products in runs of single CTAs and of few rows."""
+    rng = np.random.default_rng(15)
+    _, _, a = _weights(rng, 10100, 2100)
+    _, _, b = _weights(rng, 39000, 512)
+    x = [torch.randn(700, 2100, device="cuda").bfloat16(), torch.randn(650, 2100, device="cuda").bfloat16(), torch.randn(20, 512, device="cuda"),
+         torch.randn(3, 512, device="cuda")]
+    m = [a, a, b, b]
+    want = [ts.ts_mxfp4_product(w, v) for w, v in zip(m, x)]
+    streams, ws = [torch.cuda.Stream() for _ in range(3)], [w.workspace(v.shape[0], v.dtype) for w, v in zip(m, x)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for i in range(4):
+            got.append(ts.ts_mxfp4_product(m[i], x[i], workspace=ws[i], stream=streams[min(i, 2)]))
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+    for i, y in enumerate(got):
+        assert torch.equal(y, want[i % 4])
