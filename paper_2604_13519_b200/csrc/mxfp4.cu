@@ -406,14 +406,6 @@ int mx_weight_map(CUtensorMap *map, const void *data, uint64_t blocks) {
   return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 3, const_cast<void *>(data), dims, strides, box, es,
                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
-int mx_rows_map(CUtensorMap *map, const void *data, uint64_t rows, int box_rows) {
-  const EncodeTiledFn encode = encode_fn();
-  if (!encode) return CUDA_ERROR_NOT_FOUND;
-  const cuuint64_t dims[2] = {128, rows}, strides[1] = {128};
-  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, es[2] = {1, 1};
-  return (int)encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(data), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                     CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-}
 
 }  // namespace ts
 

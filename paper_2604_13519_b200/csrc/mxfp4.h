@@ -33,8 +33,7 @@ struct MxArgs {
   int tiles, n_kb;           // 128-row tiles and 128-column blocks of the matrix
   int planes;                // planes of e4m3 numbers that are added
   int early;                 // the matrix was written long ago: its blocks may be fetched before the previous kernel is done
-  int Mc, chunks, stages, n_acc, sets;   // filled in by the launcher: activation rows per tile of the result, their chunks, stages of the ring,
-                                         // accumulators, scales of so many blocks in tensor memory
+  int Mc, chunks, stages, n_acc;   // filled in by the launcher: activation rows per tile of the result, their chunks, stages of the ring, accumulators
   long long units;           // tiles x chunks x k-blocks
   int *err;                  // device status word (null: not wanted)
   unsigned long long *stamp;
@@ -231,10 +230,10 @@ template <int EPI> __device__ __forceinline__ void mx_finish(const MxArgs &g, lo
 #endif
 
 // How a product is dealt out: activation rows per chunk (a multiple of 8, planes x rows one of 16), chunks; runs of k-blocks
-// (stream; apart: a launch per chunk; pairs: to pairs of CTAs) or a tile to each of `ctas` clusters; whether it makes the planes itself.
-struct MxPlan { int Mc, chunks, ctas, cluster; bool stream, apart, own, pairs; };
-// fits[c]: clusters of c CTAs that the device runs at once, two CTAs to an SM, fits[0]: pairs of one to an SM (mx_fits); null: none are made.  alone: no kernel
-// before the product could leave the planes.
+// (stream; apart: a launch per chunk) or a tile to each of `ctas` clusters; whether it makes the planes itself.
+struct MxPlan { int Mc, chunks, ctas, cluster; bool stream, apart, own; };
+// fits[c]: clusters of c CTAs that the device runs at once, two CTAs to an SM (mx_fits); null: none are made.  alone: no kernel before the product
+// could leave the planes.
 MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits, bool alone);
 void mx_fits(int (&fits)[9]);
 
@@ -269,8 +268,6 @@ cudaError_t launch_mx_dequantise(const uint8_t *codes, const uint8_t *scales, in
 cudaError_t launch_mx_lay_out(const uint8_t *codes, const uint8_t *scales, int n_rows, int r0, int nb, RowMap rm, uint8_t *w, cudaStream_t st);
 // The descriptor of a laid-out matrix of `blocks` blocks; returns a CUresult.
 int mx_weight_map(CUtensorMap *map, const void *data, uint64_t blocks);
-// ... of `rows` rows of 128 bytes, copied `box` at a time as they are
-int mx_rows_map(CUtensorMap *map, const void *data, uint64_t rows, int box);
 
 // Planes (mx_planes8_kernel) lie in blocks as the product's shared memory holds them: [chunk of Mc rows][128 columns] { elements [column c
 // of the instruction = plane * Mc + row][128 bytes, 16-byte pieces swizzled: piece ^ (c & 7)], scales [c / 128][lane c % 32]

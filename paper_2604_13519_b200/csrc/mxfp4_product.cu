@@ -11,7 +11,7 @@
 // shared into tensor memory (tcgen05.cp: 32 lanes x 16 bytes, repeated in all four lane quarters): word j of lane l = the four scales
 // of row 32 j + l along a block's 128 columns.
 //
-// Three ways to deal the work out; which one a product takes depends on its tiles alone (128 features x a chunk of rows).
+// Two ways to deal the work out; which one a product takes depends on its tiles alone (128 features x a chunk of rows).
 //
 // kStream, for more tiles than CTAs fit: in k-blocks.  (tile, k-block) pairs in order, an equal run of them to each of two CTAs per SM, so
 // that all SMs stream the same bytes whatever the matrix's shape and a launch has one start and one end.  A CTA walks its run from the
@@ -23,18 +23,14 @@
 // Otherwise one tile to a CTA, or, where that leaves places empty, to a cluster of CTAs along K, whose sums meet through
 // distributed shared memory: less of an exchange than through L2, which counts where a CTA has few k-blocks.
 //
-// kPairs, for many rows: runs as above, dealt out to pairs of CTAs (one to an SM) on two tiles of features.  Each keeps its own tile's weights and
-// half of the activations, which the instruction (cta_group::2) multiplies with both, so that a block's activations come out of L2 once for
-// two tiles and an SM's shared memory is busy for 256 + columns cycles with a block instead of 256 + 2 x columns.  The first CTA of a pair issues for both, and both
-// CTAs' copies count on its barriers: tensor copies all of them, since others can only count on barriers of their own CTA.  (A warp of the
-// second CTA that passed the word on, with an arrival that releases at cluster scope, took 1500 cycles per block.)
+// Up to two rows, four or eight where a CTA has few blocks (mx_plan), CTAs that have a tile each make the planes themselves (kTile with
+// kOwn): four more warps turn a stage's 128 columns into e4m3 on the way into shared memory, which saves a launch; for more rows a kernel
+// ahead does it once for all CTAs (launch_mx_input).
 //
-// Up to two or four rows CTAs that have a tile each make the planes themselves (kTile with kOwn): four more warps turn a stage's 128 columns into e4m3
-// on the way into shared memory, which saves a launch; for more rows a kernel ahead does it once for all CTAs (launch_mx_input).
-//
-// Roles: warp 0 = copies, warp 1 = tensor memory, scales and products, warps 2..5 = epilogue, warps 6.. = planes (kOwn).  Pairs, which have an SM
-// to themselves: warps 2..9 = epilogue, warp 10 = copies of activations.
-// Every wait is bounded; on expiry the CTA records an error word and leaves through the normal exit.
+// Roles: warp 0 = copies, warp 1 = tensor memory, scales and products, warps 2..5 = epilogue, warps 6.. = planes (kOwn).
+// Every wait on a barrier or a flag is bounded; on expiry the CTA records an error word and leaves through the normal exit.  Waits that have
+// no bounded form: tcgen05.alloc (an SM holds two of these CTAs by their shared memory, each with half of the tensor memory at most), the
+// cluster barriers (every thread reaches them through bounded waits) and the dependency wait.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -47,9 +43,9 @@ static constexpr int kProdMaxStages = 12;
 static constexpr int kProdW = kMxTileN * kMxTileK;   // a block's elements in shared memory
 static constexpr int kProdStaging = 2 * 8 * kMxTileN * 4;   // eight rows of sums, twice
 static constexpr int kProdAcc = 224;                  // most columns of an accumulator: with 24 of scales (two stages) half of the tensor memory
-static constexpr int kProdCtas = 2;                   // per SM (kPairs: one, all of the tensor memory)
+static constexpr int kProdCtas = 2;                   // per SM
 
-enum : int { kTile = 0, kStream = 1, kPairs = 2 };
+enum : int { kTile = 0, kStream = 1 };
 
 struct __align__(16) ProdSmemCtl {
   uint64_t full[kProdMaxStages];
@@ -63,38 +59,13 @@ struct __align__(16) ProdSmemCtl {
 __device__ __forceinline__ void prod_error(const MxArgs &g, int code) { if (g.err) atomicExch(g.err, code); }
 
 // D[tmem] (+)= (A x scales) * (B x scales), A e2m1 and B e4m3 in shared memory, K = 32
-template <bool kPair>
 __device__ __forceinline__ void umma_mx(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
                                         uint32_t accumulate) {
-  if constexpr (kPair)
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
-        : "memory");
-  else
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
-        : "memory");
-}
-// Arrives at the barrier (kPair: of both CTAs) when all products issued so far are done
-template <bool kPair> __device__ __forceinline__ void prod_commit(uint32_t bar) {
-  if constexpr (kPair)
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3)
-                 : "memory");
-  else
-    umma_commit(bar);
-}
-// at a barrier of the pair's first CTA
-__device__ __forceinline__ void arrive_first(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr(bar, 0)) : "memory");
-}
-template <bool kPair> __device__ __forceinline__ bool prod_wait(uint32_t bar, uint32_t parity) {
-  if constexpr (kPair) return mbar_wait_cluster(bar, parity);
-  else return mbar_wait(bar, parity);
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+      : "memory");
 }
 // Instruction descriptor: A e2m1, B e4m3, both K-major, scales ue8m0, D fp32, M x N; the scales' byte within their words is added (see
 // mx_scale_byte)
@@ -103,23 +74,9 @@ __device__ __forceinline__ uint32_t umma_idesc_mx(uint32_t M, uint32_t N) {
 }
 __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t i) { return (i << 4) | (i << 29); }
 
-// 32 x 16 bytes of shared memory -> four columns of all four lane quarters (kPair: in both CTAs, from each one's own)
-template <bool kPair> __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
-  if constexpr (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-}
-template <bool kPair> __device__ __forceinline__ void prod_tmem_alloc(uint32_t smem_dst, uint32_t ncols) {
-  if constexpr (kPair) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(ncols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-  } else {
-    tmem_alloc(smem_dst, ncols);
-    tmem_relinquish();
-  }
-}
-template <bool kPair> __device__ __forceinline__ void prod_tmem_dealloc(uint32_t taddr, uint32_t ncols) {
-  if constexpr (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-  else tmem_dealloc(taddr, ncols);
+// 32 x 16 bytes of shared memory -> four columns of all four lane quarters
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 // no swizzle, 8 rows x 16 bytes contiguous, the next 8 rows 128 bytes further on
 __device__ __forceinline__ uint64_t scales_desc(uint32_t saddr) {
@@ -161,32 +118,17 @@ __device__ __forceinline__ bool wait_flag(const int *p) {
   }
 }
 
-// Tensor copies into this CTA's shared memory that count on a barrier of either CTA of the pair
-__device__ __forceinline__ void pair_load_2d(uint32_t dst, const void *tmap, int row, uint32_t bar, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4}], [%2], %5;"
-      ::"r"(dst), "l"(tmap), "r"(bar), "r"(0), "r"(row), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void pair_load_3d(uint32_t dst, const void *tmap, int z, uint32_t bar, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;"
-      ::"r"(dst), "l"(tmap), "r"(bar), "r"(0), "r"(0), "r"(z), "l"(policy)
-      : "memory");
-}
-
 // A block's scales into tensor memory (at `sf`) and its products.  A copy waits for nothing that was issued before it, so a stage of the
 // ring has columns of its own for its scales: by the time that its barrier says full again, the products that read them are done.
-template <bool kPair>
 __device__ __forceinline__ void prod_block(uint32_t sa, uint32_t sf, uint32_t d, uint32_t idesc, int act_bytes, int sb_words, bool accumulate) {
   const uint32_t sx = sa + kProdW, sfx = sx + act_bytes, sfw = sfx + 512 * sb_words;
-  tmem_cp_scales<kPair>(sf, scales_desc(sfw));
-  tmem_cp_scales<kPair>(sf + 4, scales_desc(sfx));
-  if (sb_words > 1) tmem_cp_scales<kPair>(sf + 8, scales_desc(sfx + 512));
+  tmem_cp_scales(sf, scales_desc(sfw));
+  tmem_cp_scales(sf + 4, scales_desc(sfx));
+  if (sb_words > 1) tmem_cp_scales(sf + 8, scales_desc(sfx + 512));
   const uint64_t da = umma_desc_sw128(sa), db = umma_desc_sw128(sx);
 #pragma unroll
   for (int kk = 0; kk < kMxTileK / 32; ++kk)   // 32 elements along K are 32 bytes of a row
-    umma_mx<kPair>(d, da + 2 * kk, db + 2 * kk, idesc | mx_scale_byte(kk), sf, sf + 4, accumulate || kk != 0);
+    umma_mx(d, da + 2 * kk, db + 2 * kk, idesc | mx_scale_byte(kk), sf, sf + 4, accumulate || kk != 0);
 }
 
 // eight rows' sums of this thread's feature, planes added
@@ -209,100 +151,66 @@ __device__ __forceinline__ void prod_sums(const MxArgs &g, uint32_t taddr, float
 
 // kOwn: pairs of rows whose planes the CTA makes, 0: none
 __host__ __device__ constexpr int own_warps(int own) { return own == 0 ? 0 : 4; }
-// Tensor maps of a launch: the weights' elements, and for pairs, as rows of 128 bytes, the weights' scales, the activations' elements (half a
-// block at a time) and their scales.
-template <bool kPair> struct ProdMaps { CUtensorMap w; };
-template <> struct ProdMaps<true> { CUtensorMap w, ws, x, xs; };
-template <int MODE, int kOwn> __host__ __device__ constexpr int prod_threads() { return 192 + (MODE == kPairs ? 160 : 32 * own_warps(kOwn)); }
-__host__ __device__ constexpr int prod_staging(bool pair) { return pair ? 2 * kProdStaging : kProdStaging; }
+template <int kOwn> __host__ __device__ constexpr int prod_threads() { return 192 + 32 * own_warps(kOwn); }
 
 template <int EPI, int MODE, int kOwn, int TYPE>
-__global__ void __launch_bounds__(prod_threads<MODE, kOwn>(), MODE == kPairs ? 1 : kProdCtas)
-mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const MxArgs g) {
+__global__ void __launch_bounds__(prod_threads<kOwn>(), kProdCtas)
+mx_product_kernel(const __grid_constant__ CUtensorMap tw, const MxArgs g) {
   extern __shared__ __align__(1024) uint8_t smem[];
-  constexpr bool kRuns = MODE != kTile, kPair = MODE == kPairs;
+  constexpr bool kRuns = MODE == kStream;
   const int ncols = g.planes * g.Mc, sb_words = (ncols + 127) / 128;   // (512 bytes of scales for 128 columns)
-  const int act_all = ncols * kMxTileK, act_bytes = kPair ? act_all / 2 : act_all, scale_bytes = 512 * (1 + sb_words);
+  const int act_bytes = ncols * kMxTileK, scale_bytes = 512 * (1 + sb_words);
   const int stage_bytes = kProdW + ((act_bytes + scale_bytes + 1023) & ~1023);
   uint8_t *staging = smem + (size_t)g.stages * stage_bytes;
-  ProdSmemCtl *ctl = reinterpret_cast<ProdSmemCtl *>(staging + prod_staging(kPair));
+  ProdSmemCtl *ctl = reinterpret_cast<ProdSmemCtl *>(staging + kProdStaging);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kCtas = kPair ? 2 : 1;        // that share a run: rank r has tile kCtas * t + r, and slabs and flags of its own
-  const int rank = kPair ? blockIdx.x & 1 : 0, cta = blockIdx.x / kCtas, G = gridDim.x / kCtas;
+  const int cta = blockIdx.x, G = gridDim.x;
   const int split = blockIdx.y, C = kRuns ? 1 : (int)gridDim.y;   // the CTA's rank in its cluster, which spans the K slices of a tile
   const long long first = (long long)cta * g.n_kb;   // (one tile: cta is the item)
   const long long u0 = kRuns ? prod_start(g, cta, G) : first + (long long)split * g.n_kb / C;
   const long long u1 = kRuns ? prod_start(g, cta + 1, G) : first + (long long)(split + 1) * g.n_kb / C;
   const uint32_t acc_cols = (ncols + 31) & ~31u, n_acc = g.n_acc, scales_at = n_acc * acc_cols, set_cols = 4 + 4 * sb_words;
   uint32_t alloc_cols = 64;
-  while (alloc_cols < scales_at + g.sets * set_cols) alloc_cols <<= 1;
+  while (alloc_cols < scales_at + g.stages * set_cols) alloc_cols <<= 1;
 
   if (warp == 0 && lane == 0) {
-    tma_prefetch_desc(&maps.w);
-    if constexpr (kPair) {
-      tma_prefetch_desc(&maps.ws);
-      tma_prefetch_desc(&maps.x);
-      tma_prefetch_desc(&maps.xs);
-    }
+    tma_prefetch_desc(&tw);
     for (int s = 0; s < g.stages; ++s) {
-      mbar_init(smem_u32(&ctl->full[s]), kOwn || kPair ? 2 : 1);   // the copies (and a warp of planes; two warps' copies)
+      mbar_init(smem_u32(&ctl->full[s]), kOwn ? 2 : 1);   // the copies (and a warp of planes)
       mbar_init(smem_u32(&ctl->empty[s]), 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(smem_u32(&ctl->acc_full[b]), 1);
-      mbar_init(smem_u32(&ctl->acc_empty[b]), kPair ? 16 : 4);   // (epilogue warps)
+      mbar_init(smem_u32(&ctl->acc_empty[b]), 4);   // (epilogue warps)
     }
     ctl->abort_flag = 0;
     fence_barrier_init();
   }
   if (warp == 1) {
-    prod_tmem_alloc<kPair>(smem_u32(&ctl->tmem_base), alloc_cols);
+    tmem_alloc(smem_u32(&ctl->tmem_base), alloc_cols);
+    tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
-  if constexpr (kPair) {   // (the other one's barriers are there)
-    cluster_arrive();
-    cluster_wait();
-  }
   tc_fence_after();
   const uint32_t tmem_base = ctl->tmem_base, scales = tmem_base + scales_at;
   if (threadIdx.x == 0) stamp_min(g.stamp);
   // (placed after this CTA holds its resources, so a waiting dependent can never starve an earlier kernel)
   pdl_launch_dependents();
 
-  if (warp == 0 || (kPair && warp == 10)) {
+  if (warp == 0) {
     // ------------------------------------------------------------------ copies
     // The whole warp walks the loop; one elected lane issues a stage's copies (from a lane in a branch of its own each takes twice as
     // long, and this warp's time per stage is what bounds a CTA).
     // (weights that every chunk reads again stay in L2: 1024 x 24576 x 4096 176 -> 165 us, call after call 210 -> 190)
     const uint64_t pol_w = g.chunks > 1 ? policy_evict_normal() : policy_evict_first(), pol_a = policy_evict_last();
-    const int n = (int)(u1 - u0), x_block = act_all + 512 * sb_words;
-    const bool weights = !kPair || warp == 0, activations = !kOwn && (!kPair || warp == 10);   // this warp's
-    const auto tile_of = [&](int item) { return min(item / g.chunks * kCtas + rank, g.tiles - 1); };   // (a pair's second tile may not be there)
+    const int n = (int)(u1 - u0), x_block = act_bytes + 512 * sb_words;
     auto load_w = [&](uint32_t dst, uint32_t bar, int blk) {
-      const uint32_t ws = dst + kProdW + act_bytes + 512 * sb_words;
-      if constexpr (kPair) {
-        if (rank == 0) mbar_expect_tx(bar, 2 * (kMxCodeBytes + 512));
-        bar = cluster_addr(bar, 0);
-        pair_load_3d(dst, &maps.w, blk, bar, pol_w);
-        pair_load_2d(ws, &maps.ws, blk * (kMxTileBytes / 128) + kMxCodeBytes / 128, bar, pol_w);
-      } else {
-        mbar_expect_tx(bar, kMxCodeBytes + (kOwn ? 512 : act_bytes + scale_bytes));   // (a copy that widens counts the bytes it reads)
-        tma_load_3d(dst, &maps.w, 0, 0, blk, bar, pol_w);
-        bulk_load(ws, g.w + (size_t)blk * kMxTileBytes + kMxCodeBytes, 512, bar, pol_w);
-      }
+      mbar_expect_tx(bar, kMxCodeBytes + (kOwn ? 512 : act_bytes + scale_bytes));   // (a copy that widens counts the bytes it reads)
+      tma_load_3d(dst, &tw, 0, 0, blk, bar, pol_w);
+      bulk_load(dst + kProdW + act_bytes + 512 * sb_words, g.w + (size_t)blk * kMxTileBytes + kMxCodeBytes, 512, bar, pol_w);
     };
-    auto load_x = [&](uint32_t dst, uint32_t bar, int blk) {
-      if constexpr (kPair) {   // half of the columns, all scales
-        if (rank == 0) mbar_expect_tx(bar, 2 * (act_bytes + 512 * sb_words));
-        bar = cluster_addr(bar, 0);
-        const int row = blk * (x_block / 128);
-        pair_load_2d(dst + kProdW, &maps.x, row + rank * (ncols / 2), bar, pol_a);
-        pair_load_2d(dst + kProdW + act_bytes, &maps.xs, row + ncols, bar, pol_a);
-      } else {
-        bulk_load(dst + kProdW, (const uint8_t *)g.x + (size_t)blk * x_block, x_block, bar, pol_a);
-      }
-    };
+    auto load_x = [&](uint32_t dst, uint32_t bar, int blk) { bulk_load(dst + kProdW, (const uint8_t *)g.x + (size_t)blk * x_block, x_block, bar, pol_a); };
     // weights do not depend on the previous kernel, unless it laid them out: they are on their way before the programmatic-dependency wait
     if (!g.early) pdl_wait();
     const int pre = min(g.stages, n);
@@ -310,12 +218,12 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
       long long hi = u1;
       for (int i = 0; i < pre;) {
         const ProdSeg t = prod_seg(g, u0, hi);
-        const int tile = tile_of(t.item), z = t.item % g.chunks;
+        const int tile = t.item / g.chunks, z = t.item % g.chunks;
         for (int kb = t.kb0; kb < t.kb1 && i < pre; ++kb, ++i) {
           const uint32_t dst = smem_u32(smem) + i * stage_bytes, bar = smem_u32(&ctl->full[i]);
           if (elect_one()) {
-            if (pass == 0 && weights) load_w(dst, bar, mx_block(tile, kb, g.n_kb));
-            if (pass == 1 && activations) load_x(dst, bar, z * g.n_kb + kb);
+            if (pass == 0) load_w(dst, bar, mx_block(tile, kb, g.n_kb));
+            if (pass == 1 && !kOwn) load_x(dst, bar, z * g.n_kb + kb);
           }
           __syncwarp();
         }
@@ -331,7 +239,7 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
     bool ok = true;
     for (long long hi = u1; ok && hi > u0;) {
       const ProdSeg t = prod_seg(g, u0, hi);
-      const int tile = tile_of(t.item), z = t.item % g.chunks;
+      const int tile = t.item / g.chunks, z = t.item % g.chunks;
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
         if (it >= pre) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->empty[s]), ph ^ 1));
@@ -341,8 +249,8 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
           }
           const uint32_t bar = smem_u32(&ctl->full[s]);
           if (elect_one()) {
-            if (weights) load_w(dst, bar, mx_block(tile, kb, g.n_kb));
-            if (activations) load_x(dst, bar, z * g.n_kb + kb);
+            load_w(dst, bar, mx_block(tile, kb, g.n_kb));
+            if (!kOwn) load_x(dst, bar, z * g.n_kb + kb);
           }
           __syncwarp();
         }
@@ -351,27 +259,22 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
       }
       hi -= t.kb1 - t.kb0;
     }
-    // whatever becomes of the other roles, this CTA's shared memory stays until its last copies have arrived (a pair's, which count on the
-    // first one's barriers: until both are done)
-    for (int i = max(0, it - g.stages); rank == 0 && i < it; ++i)
+    // whatever becomes of the other roles, this CTA's shared memory stays until its last copies have arrived
+    for (int i = max(0, it - g.stages); i < it; ++i)
       if (!mbar_wait(smem_u32(&ctl->full[i % g.stages]), (i / g.stages) & 1)) break;
     __syncwarp();
-  } else if (warp == 1 && rank == 1) {
-    // (a pair's products are the first CTA's)
   } else if (warp == 1) {
     // ------------------------------------------------------------------ products
-    const uint32_t idesc = umma_idesc_mx(kCtas * kMxTileN, ncols);
+    const uint32_t idesc = umma_idesc_mx(kMxTileN, ncols);
     bool ok = true;
     int s = 0, j = 0;
     uint32_t ph = 0;
-    int set = 0, ahead = 0, done = 0;    // (pairs) columns for scales; where there are fewer than stages: blocks issued since stage `done` was filled
-    uint32_t done_ph = 0;
     for (long long hi = u1; ok && hi > u0; ++j) {
       const ProdSeg t = prod_seg(g, u0, hi);
       const int b = n_acc == 2 ? j & 1 : 0, use = n_acc == 2 ? j >> 1 : j;
       const uint32_t d = tmem_base + b * acc_cols;
       // the accumulator's previous tile has been read out
-      if (use > 0 && !__all_sync(0xffffffffu, prod_wait<kPair>(smem_u32(&ctl->acc_empty[b]), (use - 1) & 1))) {
+      if (use > 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_empty[b]), (use - 1) & 1))) {
         if (lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
         ok = false;
       }
@@ -381,26 +284,19 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
         const bool pair = g.stages >= 4 && kb + 1 < t.kb1, wrap = s + 1 == g.stages;   // (a short ring would wait for two copies)
         const int s1 = wrap ? 0 : s + 1;
         const uint32_t ph1 = wrap ? ph ^ 1 : ph;
-        ok = __all_sync(0xffffffffu, prod_wait<kPair>(smem_u32(&ctl->full[s]), ph) && (!pair || prod_wait<kPair>(smem_u32(&ctl->full[s1]), ph1)));
-        if (kPair && g.sets < g.stages) {   // the products that read the columns to be written are done
-          for (ahead += 1 + pair; ok && ahead > g.sets; --ahead) {
-            ok = __all_sync(0xffffffffu, prod_wait<kPair>(smem_u32(&ctl->empty[done]), done_ph));
-            if (++done == g.stages) { done = 0; done_ph ^= 1; }
-          }
-        }
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->full[s]), ph) && (!pair || mbar_wait(smem_u32(&ctl->full[s1]), ph1)));
         if (!ok) {
           if (lane == 0) prod_error(g, DEV_TIMEOUT_FULL);
           break;
         }
         tc_fence_after();
-        const int set0 = kPair ? set : s, set1 = !kPair ? s1 : set + 1 == g.sets ? 0 : set + 1;
         const uint32_t a0 = smem_u32(smem) + s * stage_bytes, a1 = smem_u32(smem) + s1 * stage_bytes;
         if (elect_one()) {
-          prod_block<kPair>(a0, scales + set0 * set_cols, d, idesc, act_bytes, sb_words, kb != t.kb0);
-          prod_commit<kPair>(smem_u32(&ctl->empty[s]));
+          prod_block(a0, scales + s * set_cols, d, idesc, act_bytes, sb_words, kb != t.kb0);
+          umma_commit(smem_u32(&ctl->empty[s]));
           if (pair) {
-            prod_block<kPair>(a1, scales + set1 * set_cols, d, idesc, act_bytes, sb_words, true);
-            prod_commit<kPair>(smem_u32(&ctl->empty[s1]));
+            prod_block(a1, scales + s1 * set_cols, d, idesc, act_bytes, sb_words, true);
+            umma_commit(smem_u32(&ctl->empty[s1]));
           }
         }
         __syncwarp();
@@ -408,14 +304,12 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
         if (pair) {
           s = s1;
           ph = ph1;
-          set = set1;
         }
-        if (kPair && ++set == g.sets) set = 0;
         if (++s == g.stages) { s = 0; ph ^= 1; }
       }
       if (elect_one()) {
         if (!ok) *reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) = 1;
-        prod_commit<kPair>(smem_u32(&ctl->acc_full[b]));
+        umma_commit(smem_u32(&ctl->acc_full[b]));
       }
       __syncwarp();
       hi -= t.kb1 - t.kb0;
@@ -423,13 +317,10 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
   } else if (kRuns) {
     // ------------------------------------------------------------------ epilogue of a run
     // Thread <-> feature out of tensor memory, where partial sums go to and come from a slab as they are (a warp's 32 features are a line);
-    // finished ones through shared memory, eight rows at a time, to a warp per row with four features per lane.  A pair's CTAs have two
-    // groups of four warps that take 32 rows each in turn.
-    constexpr int kGroups = kPair ? 2 : 1, kTurn = 32 * kGroups;
+    // finished ones through shared memory, eight rows at a time, to a warp per row with four features per lane.
     const int q = warp & 3;                       // TMEM lane quarter this warp may read
     const int f = q * 32 + lane;                  // this thread's feature of a tile
-    const int group = kPair ? (warp - 2) >> 2 : 0, mine = 32 * group;   // first row of this warp's
-    const uint32_t stg = smem_u32(staging) + group * kProdStaging;
+    const uint32_t stg = smem_u32(staging);
     pdl_wait();   // (flags are cleared by the kernel before; outputs may still be read by its consumers)
     if (EPI == MX_SWIGLU && blockIdx.x == 0 && warp == 2) mx_clear_flags(g.mo, lane, 32);
     int j = 0, turn = 0;
@@ -438,25 +329,24 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
       const ProdSeg t = prod_seg(g, u0, hi);
       hi -= t.kb1 - t.kb0;
       const int b = n_acc == 2 ? j & 1 : 0, use = n_acc == 2 ? j >> 1 : j;
-      const int tile = t.item / g.chunks * kCtas + rank, z = t.item % g.chunks, m0 = z * g.Mc;
-      const int M = tile < g.tiles ? min(g.Mc, g.M - m0) : 0;
+      const int tile = t.item / g.chunks, z = t.item % g.chunks, m0 = z * g.Mc, M = min(g.Mc, g.M - m0);
       const bool finish = t.kb1 == g.n_kb;   // else another CTA finishes the tile
       int before = cta;                      // CTAs [before, cta) have its earlier k-blocks
       bool there = true;                     // their partial sums are
-      if (finish && M > 0 && t.kb0 > 0) {
+      if (finish && t.kb0 > 0) {
         const long long first = (long long)t.item * g.n_kb;
         do --before;
         while (prod_start(g, before, G) > first);
-        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, ld_acquire(g.flags + kCtas * c + rank));
+        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, ld_acquire(g.flags + c));
       }
       // The CTAs' partial sums, 32 rows ahead of use: the first of them are under way while the tile's last products run, unless they are late (as
-      // they are where a run is shorter than a tile).  With eight rows ahead the end of a pair's run took 12 us longer where it had any to fetch.
+      // they are where a run is shorter than a tile).
       float part[4][8];
       auto fetch = [&](int c0, float (&p)[8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] = 0.f;
         for (int c = before; there && c0 < M && c < cta; ++c) {
-          const float *slab = g.slabs + ((size_t)(kCtas * c + rank) * g.Mc + c0) * kMxTileN + f;
+          const float *slab = g.slabs + ((size_t)c * g.Mc + c0) * kMxTileN + f;
           if (c == before) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) p[i] = __ldcg(slab + i * kMxTileN);
@@ -468,17 +358,17 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
       };
       if (there) {
 #pragma unroll
-        for (int h = 0; h < 4; ++h) fetch(mine + 8 * h, part[h]);
+        for (int h = 0; h < 4; ++h) fetch(8 * h, part[h]);
       }
       bool ok = alive && __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_full[b]), use & 1));
       if (alive && !ok && lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
       alive = ok;
       if (!there) {
         there = ok;
-        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, wait_flag(g.flags + kCtas * c + rank));
+        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, wait_flag(g.flags + c));
         if (ok && !there && lane == 0) prod_error(g, DEV_TIMEOUT_GRID);
 #pragma unroll
-        for (int h = 0; h < 4; ++h) fetch(mine + 8 * h, part[h]);
+        for (int h = 0; h < 4; ++h) fetch(8 * h, part[h]);
       }
       tc_fence_after();
       ok = ok && there && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
@@ -486,31 +376,25 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
       auto emptied = [&]() {   // the sums are out of tensor memory
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          if constexpr (kPair) arrive_first(smem_u32(&ctl->acc_empty[b]));
-          else mbar_arrive(smem_u32(&ctl->acc_empty[b]));
-        }
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[b]));
       };
-      if (mine >= M) emptied();   // (no rows of this warp's)
       if (!finish) {
-        if (M == 0) continue;
-        float *slab = g.slabs + (size_t)blockIdx.x * g.Mc * kMxTileN + f;
-        for (int r0 = mine; r0 < M; r0 += kTurn)
-          for (int c0 = r0; c0 < min(M, r0 + 32); c0 += 8) {
-            float v[8];
-            prod_sums(g, taddr + c0, v);
-            if (c0 + 8 >= min(M, r0 + 32) && r0 + kTurn >= M) emptied();
+        float *slab = g.slabs + (size_t)cta * g.Mc * kMxTileN + f;
+        for (int c0 = 0; c0 < M; c0 += 8) {
+          float v[8];
+          prod_sums(g, taddr + c0, v);
+          if (c0 + 8 >= M) emptied();
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (ok) __stcg(slab + (c0 + i) * kMxTileN, v[i]);   // (rows behind the last one too: Mc is a multiple of eight)
-          }
+          for (int i = 0; i < 8; ++i)
+            if (ok) __stcg(slab + (c0 + i) * kMxTileN, v[i]);   // (rows behind the last one too: Mc is a multiple of eight)
+        }
         __threadfence();
-        asm volatile("bar.sync 1, %0;" ::"n"(128 * kGroups) : "memory");
-        if (warp == 2 && lane == 0 && ok) asm volatile("st.release.gpu.global.b32 [%0], %1;" ::"l"(g.flags + blockIdx.x), "r"(1) : "memory");
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (warp == 2 && lane == 0 && ok) asm volatile("st.release.gpu.global.b32 [%0], %1;" ::"l"(g.flags + cta), "r"(1) : "memory");
         continue;
       }
       const int n = tile * kMxTileN + lane * 4;
-      for (int r0 = mine; r0 < M; r0 += kTurn) {
+      for (int r0 = 0; r0 < M; r0 += 32) {
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           const int c0 = r0 + 8 * h;
@@ -519,11 +403,11 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
           turn ^= 1;
           float v[8];
           prod_sums(g, taddr + c0, v);
-          if ((h == 3 || c0 + 8 >= M) && r0 + kTurn >= M) emptied();
+          if (c0 + 8 >= M) emptied();
 #pragma unroll
           for (int i = 0; i < 8; ++i) st_shared_f32(buf + (i * kMxTileN + f) * 4, v[i] + part[h][i]);
-          fetch(c0 + kTurn, part[h]);
-          asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory");
+          fetch(c0 + 32, part[h]);
+          asm volatile("bar.sync 2, 128;" ::: "memory");
           for (int i = q; ok && i < 8 && c0 + i < M; i += 4) {
             const uint4 u = ld_shared_v4(buf + (i * kMxTileN + lane * 4) * 4);
             const float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
@@ -617,12 +501,6 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
       if (lane == 0) mbar_arrive(smem_u32(&ctl->full[s]));
     }
   }
-  if constexpr (kPair) {
-    // (products and barriers of either are in the other one's memory until both are done)
-    __syncwarp();
-    cluster_arrive();
-    cluster_wait();
-  }
   if constexpr (!kRuns) {
     if (C > 1) {
       // (every thread of the cluster takes part in both barriers: the sums are in shared memory, then: nobody reads mine any more)
@@ -639,16 +517,13 @@ mx_product_kernel(const __grid_constant__ ProdMaps<MODE == kPairs> maps, const M
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    prod_tmem_dealloc<kPair>(tmem_base, alloc_cols);
+    tmem_dealloc(tmem_base, alloc_cols);
   }
   if (threadIdx.x == 0 && g.stamp) stamp_max(g.stamp + 3);
 }
 
 // (elements of the weights, their scales, the activations' block as it lies in memory: both operands on 1024-byte boundaries)
-static size_t prod_stage_bytes(int planes, int Mc, bool pairs) {
-  const int ncols = planes * Mc;
-  return kProdW + ((512 + mx_x_block(ncols) - (pairs ? ncols * kMxTileK / 2 : 0) + 1023) & ~1023);
-}
+static size_t prod_stage_bytes(int planes, int Mc) { return kProdW + ((512 + mx_x_block(planes * Mc) + 1023) & ~1023); }
 
 // Rows per chunk: all of them up to 224 instruction columns, else equal chunks of fewer.  Then CTAs, two to an SM: clusters of as many
 // along K as there is room for, eight at most, or runs of k-blocks.  Up to 64 rows (fp32: 32, which is a chunk) neither the cut along K nor
@@ -665,43 +540,20 @@ static size_t prod_stage_bytes(int planes, int Mc, bool pairs) {
 // and 8.8), but cost a call of its own one launch less on the host (12.3 -> 9.5 us).
 constexpr int kOwnRows = 2, kOwnRowsShort = 4, kOwnRowsAlone = 8, kOwnShort = 8;
 constexpr int kRunCycles = 25000;
-// Equal chunks of at most `cols` instruction columns (planes x rows), of which there are a multiple of 16, with pairs of CTAs of 32.
-static int mx_step(int planes, bool pairs) { return pairs ? (planes % 4 == 0 ? 8 : planes % 2 == 0 ? 16 : 32) : planes % 2 ? 16 : 8; }
-static MxPlan mx_cut(int M, int planes, bool pairs, int cols) {
+// Equal chunks of at most kProdAcc instruction columns (planes x rows), of which there are a multiple of 16.
+static int mx_step(int planes) { return planes % 2 ? 16 : 8; }
+static MxPlan mx_cut(int M, int planes) {
   MxPlan p{};
-  const int step = mx_step(planes, pairs), most = cols / planes / step * step;
-  p.pairs = pairs;
+  const int step = mx_step(planes), most = kProdAcc / planes / step * step;
   p.chunks = (M + most - 1) / most;
   p.Mc = ((M + p.chunks - 1) / p.chunks + step - 1) / step * step;
   p.chunks = (M + p.Mc - 1) / p.Mc;
   return p;
 }
-// A pair of CTAs takes 250 ns for a block of 256 x 128 at 128 columns, 273 at 160, 295 at 192 and 374 at 224, where the ring has six stages and not
-// seven: chunks of up to 192 columns but where ones of 224 are as much fewer.
-constexpr int kPairCols = 192;
-static MxPlan mx_cut_pairs(int M, int planes) {
-  const MxPlan a = mx_cut(M, planes, true, kPairCols), b = mx_cut(M, planes, true, kProdAcc);
-  const auto ns = [&](const MxPlan &p) { return p.chunks * (planes * p.Mc > kPairCols ? 374 : 160 + planes * p.Mc * 7 / 10); };
-  return ns(b) < ns(a) ? b : a;
-}
-// Pairs take about 7 us longer than the other ways from a launch's start to its end, and from some 70 blocks a pair on that is less than what
-// they save: 1024 rows x 4096 x 4096 (76 blocks) 55 -> 43 us, 128 x 24576 x 4096 (83) 44 -> 37, 512 x 6144 x 4096 (62) 33 and 37, 1024 x 24576 x 4096
-// 197 -> 187, 96 x 151936 x 4096 140 -> 102, 1000 x 4096 x 4096 of fp32 98 -> 79.
-constexpr int kPairBlocks = 70;
 MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fits, bool alone) {
-  MxPlan p = mx_cut(M, planes, false, kProdAcc);
+  MxPlan p = mx_cut(M, planes);
   n_sms = std::min(n_sms, kMxMostSms);
   const bool same = M <= (planes == 5 ? 32 : 64);
-  if (!same && fits && fits[0]) {
-    MxPlan q = mx_cut_pairs(M, planes);
-    const int pairs = std::min(fits[0], n_sms / 2);
-    if ((tiles + 1) / 2 * (long long)q.chunks * n_kb >= (long long)kPairBlocks * pairs) {
-      q.stream = true;
-      q.cluster = 1;
-      q.ctas = 2 * pairs;
-      return q;
-    }
-  }
   const long long items = (long long)tiles * (same ? 1 : p.chunks), places = (long long)kProdCtas * n_sms;
   const long long uneven = ((items + n_sms - 1) / n_sms * n_sms - items) * n_kb * (256 + 2 * 32) / n_sms;
   p.apart = same && p.chunks > 1;
@@ -727,30 +579,25 @@ MxScratch mx_scratch(int n_kb, int planes, const MxPlan &p) {
 }
 uint64_t mx_scratch_most(int rows, int n_kb, int planes) {
   if (!rows || !n_kb) return 0;
-  uint64_t most = 0;
-  for (const int cols : {kProdAcc, kPairCols})
-    for (const bool pairs : {false, true}) {
-      MxPlan p = mx_cut(rows, planes, pairs, cols);
-      if (p.chunks > 1) {   // (equal chunks may be larger for fewer rows)
-        p.Mc = cols / planes / mx_step(planes, pairs) * mx_step(planes, pairs);
-        p.chunks = (rows + p.Mc - 1) / p.Mc;
-      }
-      p.stream = p.apart = true;
-      p.ctas = kProdCtas * kMxMostSms;
-      most = std::max(most, mx_scratch(n_kb, planes, p).bytes);
-    }
-  return most;
+  MxPlan p = mx_cut(rows, planes);
+  if (p.chunks > 1) {   // (equal chunks may be larger for fewer rows)
+    p.Mc = kProdAcc / planes / mx_step(planes) * mx_step(planes);
+    p.chunks = (rows + p.Mc - 1) / p.Mc;
+  }
+  p.stream = p.apart = true;
+  p.ctas = kProdCtas * kMxMostSms;
+  return mx_scratch(n_kb, planes, p).bytes;
 }
 
-static constexpr size_t kProdSmem = 113 * 1024, kPairSmem = 227 * 1024;   // of a CTA
+static constexpr size_t kProdSmem = 113 * 1024;   // of a CTA
 int gemm_max_clusters(int cluster, size_t smem_budget);   // gemm_tcgen05.cu
 void mx_fits(int (&fits)[9]) {
-  fits[0] = gemm_max_clusters(2, kPairSmem);
+  fits[0] = 0;
   for (int c = 1; c <= 8; ++c) fits[c] = gemm_max_clusters(c, kProdSmem);
 }
 
 template <int EPI, int MODE, int kOwn, int TYPE>
-static cudaError_t prod_launch_one(const ProdMaps<true> &maps, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
+static cudaError_t prod_launch_one(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
   static PerDeviceOnce once;
   int dev = -1;
   if (once.needed(&dev)) {
@@ -760,14 +607,14 @@ static cudaError_t prod_launch_one(const ProdMaps<true> &maps, const MxArgs &g, 
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(p.ctas, p.cluster);
-  cfg.blockDim = dim3(prod_threads<MODE, kOwn>());
+  cfg.blockDim = dim3(prod_threads<kOwn>());
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   int n = 0;
-  if (p.cluster > 1 || MODE == kPairs) {
+  if (p.cluster > 1) {
     at[n].id = cudaLaunchAttributeClusterDimension;
-    at[n].val.clusterDim.x = MODE == kPairs ? 2 : 1;
+    at[n].val.clusterDim.x = 1;
     at[n].val.clusterDim.y = p.cluster;
     at[n].val.clusterDim.z = 1;
     ++n;
@@ -779,27 +626,25 @@ static cudaError_t prod_launch_one(const ProdMaps<true> &maps, const MxArgs &g, 
   }
   cfg.attrs = at;
   cfg.numAttrs = n;
-  if constexpr (MODE == kPairs) return cudaLaunchKernelEx(&cfg, mx_product_kernel<EPI, MODE, kOwn, TYPE>, maps, g);
-  else return cudaLaunchKernelEx(&cfg, mx_product_kernel<EPI, MODE, kOwn, TYPE>, ProdMaps<false>{maps.w}, g);
+  return cudaLaunchKernelEx(&cfg, mx_product_kernel<EPI, MODE, kOwn, TYPE>, tw, g);
 }
 
 template <int EPI, int TYPE>
-static cudaError_t prod_launch_own(const ProdMaps<true> &maps, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
-  if (g.M <= 2) return prod_launch_one<EPI, kTile, 1, TYPE>(maps, g, p, smem, st, pdl);
-  if (g.M <= 4) return prod_launch_one<EPI, kTile, 2, TYPE>(maps, g, p, smem, st, pdl);
-  if constexpr (EPI == MX_STORE && TYPE == MX_BF16) return prod_launch_one<EPI, kTile, 4, TYPE>(maps, g, p, smem, st, pdl);
+static cudaError_t prod_launch_own(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
+  if (g.M <= 2) return prod_launch_one<EPI, kTile, 1, TYPE>(tw, g, p, smem, st, pdl);
+  if (g.M <= 4) return prod_launch_one<EPI, kTile, 2, TYPE>(tw, g, p, smem, st, pdl);
+  if constexpr (EPI == MX_STORE && TYPE == MX_BF16) return prod_launch_one<EPI, kTile, 4, TYPE>(tw, g, p, smem, st, pdl);
   return cudaErrorInvalidValue;
 }
 template <int EPI>
-static cudaError_t prod_launch(const ProdMaps<true> &maps, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
-  if (p.pairs) return prod_launch_one<EPI, kPairs, 0, 0>(maps, g, p, smem, st, pdl);
-  if (p.stream) return prod_launch_one<EPI, kStream, 0, 0>(maps, g, p, smem, st, pdl);
-  if (!p.own) return prod_launch_one<EPI, kTile, 0, 0>(maps, g, p, smem, st, pdl);
+static cudaError_t prod_launch(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
+  if (p.stream) return prod_launch_one<EPI, kStream, 0, 0>(tw, g, p, smem, st, pdl);
+  if (!p.own) return prod_launch_one<EPI, kTile, 0, 0>(tw, g, p, smem, st, pdl);
   switch (g.x_type) {
-    case MX_BF16: return prod_launch_own<EPI, MX_BF16>(maps, g, p, smem, st, pdl);
-    case MX_F16: return prod_launch_own<EPI, MX_F16>(maps, g, p, smem, st, pdl);
-    case MX_PAIR: return prod_launch_own<EPI, MX_PAIR>(maps, g, p, smem, st, pdl);
-    default: return prod_launch_own<EPI, MX_F32>(maps, g, p, smem, st, pdl);
+    case MX_BF16: return prod_launch_own<EPI, MX_BF16>(tw, g, p, smem, st, pdl);
+    case MX_F16: return prod_launch_own<EPI, MX_F16>(tw, g, p, smem, st, pdl);
+    case MX_PAIR: return prod_launch_own<EPI, MX_PAIR>(tw, g, p, smem, st, pdl);
+    default: return prod_launch_own<EPI, MX_F32>(tw, g, p, smem, st, pdl);
   }
 }
 
@@ -817,29 +662,19 @@ cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const Mx
   g.ldx = in.ldx; g.pair = in.pair; g.x_type = in.type; g.K = in.cols;
   g.vec_x = mx_aligned(in.x, in.ldx, in.type) && (in.type != MX_PAIR || in.pair % 8 == 0);
   g.slabs = (float *)((uint8_t *)scratch + w.slabs);
-  const size_t stage = prod_stage_bytes(g.planes, g.Mc, p.pairs), fixed = prod_staging(p.pairs) + sizeof(ProdSmemCtl);
-  g.stages = (int)std::min<size_t>(kProdMaxStages, ((p.pairs ? kPairSmem : kProdSmem) - fixed) / stage);
-  const int ncols = g.planes * g.Mc, tmem = p.pairs ? 512 : 256;
-  const int acc = (ncols + 31) & ~31, set = 4 + 4 * ((ncols + 127) / 128);   // columns of an accumulator, of a stage's scales
-  g.sets = p.pairs ? std::min(g.stages, (tmem - 2 * acc) / set) : g.stages;
-  const int sets = g.sets * set;
-  g.n_acc = p.stream && 2 * acc + sets <= tmem ? 2 : 1;
-  const size_t smem = std::max(g.stages * stage + fixed, p.pairs ? kProdSmem + 4096 : 0);   // (more than half an SM's: a pair is on two SMs)
+  const size_t stage = prod_stage_bytes(g.planes, g.Mc), fixed = kProdStaging + sizeof(ProdSmemCtl);
+  g.stages = (int)std::min<size_t>(kProdMaxStages, (kProdSmem - fixed) / stage);
+  const int ncols = g.planes * g.Mc;
+  const int acc = (ncols + 31) & ~31, sets = g.stages * (4 + 4 * ((ncols + 127) / 128));   // columns of an accumulator, of the stages' scales
+  g.n_acc = p.stream && 2 * acc + sets <= 256 ? 2 : 1;
+  const size_t smem = g.stages * stage + fixed;
   const bool apart = p.stream && p.apart;
   const int passes = apart ? p.chunks : 1;
   g.chunks = apart ? 1 : p.chunks;
-  g.units = (long long)(p.pairs ? (g.tiles + 1) / 2 : g.tiles) * g.chunks * g.n_kb;
-  if (g.stages < 2 || g.sets < std::min(3, g.stages) || g.Mc % 8 || ncols % 16 || ncols > kProdAcc || g.n_acc * acc + sets > tmem || (p.pairs && (ncols % 32 || p.ctas % 2)) || p.ctas < 1 || p.cluster < 1 || p.cluster > 8 ||
-      p.cluster > g.n_kb || (p.stream && p.ctas / (p.pairs ? 2 : 1) > g.units) || (size_t)g.stages * stage < (size_t)g.Mc * kMxTileN * 4 || (p.own && passes != 1))
+  g.units = (long long)g.tiles * g.chunks * g.n_kb;
+  if (g.stages < 2 || g.Mc % 8 || ncols % 16 || ncols > kProdAcc || g.n_acc * acc + sets > 256 || p.ctas < 1 || p.cluster < 1 || p.cluster > 8 ||
+      p.cluster > g.n_kb || (p.stream && p.ctas > g.units) || (size_t)g.stages * stage < (size_t)g.Mc * kMxTileN * 4 || (p.own && passes != 1))
     return cudaErrorInvalidValue;
-  ProdMaps<true> maps;
-  maps.w = tw;
-  if (p.pairs) {
-    const uint64_t rows_x = (uint64_t)g.chunks * g.n_kb * (mx_x_block(ncols) / 128), rows_w = (uint64_t)g.tiles * g.n_kb * (kMxTileBytes / 128);
-    if (mx_rows_map(&maps.ws, g.w, rows_w, 4) || mx_rows_map(&maps.x, scratch, rows_x, ncols / 2) ||
-        mx_rows_map(&maps.xs, scratch, rows_x, 4 * ((ncols + 127) / 128)))
-      return cudaErrorInvalidValue;
-  }
   for (int i = 0; i < passes; ++i) {
     g.row0 = i * g.Mc;
     g.M = passes == 1 ? in.rows : std::min(g.Mc, in.rows - g.row0);
@@ -847,9 +682,9 @@ cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const Mx
     g.flags = (int *)((uint8_t *)scratch + w.flags) + (p.stream ? i * p.ctas : 0);
     cudaError_t e = cudaErrorInvalidValue;
     switch (epi) {
-      case MX_STORE: e = prod_launch<MX_STORE>(maps, g, p, smem, st, pdl); break;
-      case MX_SWIGLU: e = prod_launch<MX_SWIGLU>(maps, g, p, smem, st, pdl); break;
-      case MX_LOGITS: e = prod_launch<MX_LOGITS>(maps, g, p, smem, st, pdl); break;
+      case MX_STORE: e = prod_launch<MX_STORE>(tw, g, p, smem, st, pdl); break;
+      case MX_SWIGLU: e = prod_launch<MX_SWIGLU>(tw, g, p, smem, st, pdl); break;
+      case MX_LOGITS: e = prod_launch<MX_LOGITS>(tw, g, p, smem, st, pdl); break;
     }
     if (e != cudaSuccess) return e;
   }
