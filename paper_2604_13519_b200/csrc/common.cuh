@@ -162,6 +162,10 @@ __device__ __forceinline__ void ld_global_v8(const void *p, uint32_t *r) {
                : "l"(p)
                : "memory");
 }
+// 16 bytes; `p` must be 16-byte aligned
+__device__ __forceinline__ void ld_global_v4(const void *p, uint32_t *r) {
+  asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p) : "memory");
+}
 
 // 16 / 8 bytes, or zeros where `p` is false.  (A statement of its own, so that a run of them is issued as written: under a
 // branch each the compiler made every load wait for the one before.)

@@ -71,7 +71,9 @@ template <int TYPE> __device__ __forceinline__ typename MxElem<TYPE>::raw mx_fro
   else return __float_as_uint(v);
 }
 
-// elements [c, c + 8) of a row of `cols` as they are, zeros behind its end and where `there` is false
+// elements [c, c + 8) of a row of `cols` as they are, zeros behind its end and where `there` is false.  (Coherent loads, in the order in which
+// they stand: most callers run while the kernel ahead of them still writes these rows, up to the dependency wait, and __ldg is for data that
+// nobody writes during the kernel.)
 template <int TYPE> struct MxRaw8 { uint32_t w[TYPE == MX_F32 || TYPE == MX_PAIR ? 8 : 4]; };
 template <int TYPE>
 __device__ __forceinline__ void mx_fetch8(const typename MxElem<TYPE>::raw *p, long long pair, bool there, int c, int cols, bool vec, MxRaw8<TYPE> &x) {
@@ -88,10 +90,7 @@ __device__ __forceinline__ void mx_fetch8(const typename MxElem<TYPE>::raw *p, l
         }
       }
 #pragma unroll
-      for (int i = 0; i < (TYPE == MX_F32 ? 2 : 1); ++i) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(q) + i);
-        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-      }
+      for (int i = 0; i < (TYPE == MX_F32 ? 2 : 1); ++i) ld_global_v4(reinterpret_cast<const uint4 *>(q) + i, w + 4 * i);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {

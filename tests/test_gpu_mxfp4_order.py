@@ -32,3 +32,35 @@ def test_steps_back_to_back(batch, k, act_split):
     torch.cuda.synchronize()
     assert (gm.read_logits(0, batch * k).view("u4") == want.view("u4")).all()
     gm.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("rows,n", [(1, 1024), (2, 1024), (4, 640), (8, 1024), (24, 1024), (100, 1024)])
+def test_a_product_reads_what_the_one_before_wrote(rows, n, dtype):
+    """Products in a chain, each one's result the next one's activations, over the same two buffers again and again: the same as with the
+    device waited for behind each."""
+    gen = torch.Generator("cuda").manual_seed(rows)
+    w = []
+    for _ in range(3):
+        codes = torch.randint(0, 256, (n, n // 2), dtype=torch.uint8, device="cuda", generator=gen)
+        # (elements of random sign, about 2.6 in size: a sum of n of them grows by 2.6 sqrt(n), and the scales take it back)
+        w.append(ts.Mxfp4Matrix(codes, torch.full((n, n // 32), 120, dtype=torch.uint8, device="cuda"), n))
+    start = [torch.randn(rows, n, device="cuda", generator=gen).to(dtype) for _ in range(4)]
+    ws = w[0].workspace(rows, dtype)
+
+    def run(wait):
+        a, b, out = torch.empty_like(start[0]), torch.empty_like(start[0]), []
+        for i in range(40):
+            a.copy_(start[i % 4])
+            for j in range(3):
+                ts.ts_mxfp4_product(w[(i + j) % 3], a, out=b, workspace=ws)
+                if wait:
+                    torch.cuda.synchronize()
+                a, b = b, a
+            out.append(a.clone())
+        return out
+    want, got = run(True), run(False)
+    for x in w:
+        x.check()
+    for i, (x, y) in enumerate(zip(want, got)):
+        assert torch.isfinite(x).all() and torch.equal(x, y), i
