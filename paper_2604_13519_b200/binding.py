@@ -726,7 +726,8 @@ def ts_mxfp4_dequantise(codes, scales, cols: int, dtype, out=None, stream=None):
 
 
 class Mxfp4Matrix:
-    """An MXFP4 matrix [n][k] in the form that ts_mxfp4_product reads, laid out from codes and scales (which it does not keep)."""
+    """An MXFP4 matrix [n][k] in the form that ts_mxfp4_product reads, laid out from codes and scales (which it does not keep).  The
+    constructor returns when it is laid out, so that products may run on any stream; it cannot be captured."""
 
     def __init__(self, codes, scales, k: int, stream=None):
         import torch
@@ -734,14 +735,16 @@ class Mxfp4Matrix:
         self.k, self.device, self.index = k, codes.device, codes.device.index
         size = C.c_uint64()
         _check(lib().ts_mxfp4_matrix_bytes(self.n, k, C.byref(size)))
-        self.data = _mx_empty(size.value, torch.uint8, self.device, stream)
-        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        torch.cuda.current_stream(self.device).synchronize()     # (products may run on any stream)
+        where = stream if stream is not None else torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(where):
+            self.data = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+            self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.handle = ts_mxfp4_matrix()
         with torch.cuda.device(self.index):
             _check(lib().ts_mxfp4_matrix_init(C.byref(self.handle), self.data.data_ptr(), self.n, k))
         self._status_ptr, self._handle_ref = self.status.data_ptr(), C.pointer(self.handle)
-        _on_device_of(self.index, stream, lib().ts_mxfp4_lay_out, codes.data_ptr(), scales.data_ptr(), self.n, k, self.data.data_ptr())
+        _on_device_of(self.index, where, lib().ts_mxfp4_lay_out, codes.data_ptr(), scales.data_ptr(), self.n, k, self.data.data_ptr())
+        where.synchronize()
 
     def workspace(self, rows: int, dtype, stream=None):
         """Scratch memory for products of up to `rows` rows of `dtype`, which a caller may keep; one per stream."""

@@ -64,3 +64,27 @@ def test_a_product_reads_what_the_one_before_wrote(rows, n, dtype):
         x.check()
     for i, (x, y) in enumerate(zip(want, got)):
         assert torch.isfinite(x).all() and torch.equal(x, y), i
+
+
+def test_a_matrix_may_be_used_on_any_stream_at_once():
+    """Laid out on a stream that is still busy, used on another one right behind the constructor, codes and scales let go of."""
+    n, k = 1024, 2048
+    lays, other = torch.cuda.Stream(), torch.cuda.Stream()
+    x = torch.randn(5, k, device="cuda").to(torch.bfloat16)
+    codes = torch.randint(0, 256, (n, k // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.full((n, k // 32), 120, dtype=torch.uint8, device="cuda")
+    want = ts.ts_mxfp4_product(ts.Mxfp4Matrix(codes, scales, k), x, torch.float32)
+    torch.cuda.synchronize()
+    for stream in (lays, None):
+        c, s = codes.clone(), scales.clone()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(lays if stream is not None else torch.cuda.current_stream()):
+            torch.cuda._sleep(200_000_000)      # (about a tenth of a second)
+        w = ts.Mxfp4Matrix(c, s, k, stream=stream)
+        del c, s
+        lost = [torch.zeros(n, k // 2, dtype=torch.uint8, device="cuda"), torch.zeros(n, k // 32, dtype=torch.uint8, device="cuda")]
+        y = ts.ts_mxfp4_product(w, x, torch.float32, stream=other)
+        other.synchronize()
+        assert torch.equal(y, want)
+        del lost
+    w.check()
