@@ -754,10 +754,13 @@ class Mxfp4Matrix:
         return _mx_empty(size.value, torch.uint8, self.device, stream)
 
     def check(self):
-        """Waits for the device and raises if a wait inside a product's kernel has expired since the last check."""
+        """Waits for all of the device's streams and raises if a wait inside a product's kernel has expired since the last check."""
+        import torch
+        torch.cuda.synchronize(self.device)
         code = int(self.status.item())
         if code:
             self.status.zero_()
+            torch.cuda.current_stream(self.device).synchronize()     # (a product on another stream may write it next)
             raise TsError(-6, f"a bounded device-side wait expired (code {code})")
 
 

@@ -88,3 +88,22 @@ def test_a_matrix_may_be_used_on_any_stream_at_once():
         assert torch.equal(y, want)
         del lost
     w.check()
+
+
+def test_check_waits_for_products_on_every_stream():
+    """A product on a stream that is still busy: its status word, set here behind it as an expired wait would set it, is seen, and
+    taken back before anything that comes later."""
+    codes = torch.randint(0, 256, (128, 64), dtype=torch.uint8, device="cuda")
+    w = ts.Mxfp4Matrix(codes, torch.full((128, 4), 120, dtype=torch.uint8, device="cuda"), 128)
+    x, side = torch.randn(3, 128, device="cuda"), torch.cuda.Stream()
+    for sleep, code in ((1, 0), (400_000_000, 3)):      # (the first time kernels are loaded, which the device is waited for)
+        w.check()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(sleep)
+            y = ts.ts_mxfp4_product(w, x)
+            w.status.fill_(code)
+    assert not side.query()
+    with pytest.raises(ts.TsError) as e:
+        w.check()
+    assert e.value.code == -6 and "code 3" in str(e.value)
+    w.check()
