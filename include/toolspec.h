@@ -515,8 +515,10 @@ ts_status ts_mxfp4_matrix_init(ts_mxfp4_matrix *m, const void *data, int64_t n, 
 
 /* ts_mxfp4_product: y[m][j] = sum over i of x[m][i] * W[j][i], y [rows][n] with row stride ldy, x [rows][k] with row stride ldx.
  * The tensor cores multiply the four-bit elements as they are; x goes in as a sum of 2 (bf16), 3 (fp16) or 5 (fp32) numbers of four
- * significant bits with a scale per 32 columns, which leaves out less than 2^-20 of the largest of the 32 (of bf16 and fp16 rows
- * nothing of elements down to 2^-13 of it); sums are fp32.  A row that holds an infinity or a NaN gives NaN.
+ * significant bits with a scale per 32 columns, which leaves out at most 2^-21 (bf16), 2^-25 (fp16) or 2^-33 (fp32) of the largest of
+ * the 32, or 2^-137 if that is more; of bf16 and fp16 rows nothing of elements down to 2^-13 of it.  (One bf16 element 2^14 times as large
+ * as its neighbours costs them bits, which shows where its own weight is zero.)  Sums are fp32.  A row that holds an infinity or a NaN
+ * gives NaN.
  * A row's result depends on that row and on the matrix, not on the other rows: with up to 64 rows (fp32: 32) it is the same, bit
  * for bit, whatever their number.  What lies between the rows of y is left as it is; y must not overlap x or the matrix.
  * workspace: device, 128-byte aligned, of ts_mxfp4_product_workspace bytes (host only call; enough for fewer rows too).  It holds nothing

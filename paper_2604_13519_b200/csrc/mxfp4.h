@@ -118,9 +118,9 @@ template <int TYPE> __device__ __forceinline__ void mx_widen8(const MxRaw8<TYPE>
 //
 // x as planes of e4m3 numbers (four significant bits each).  A block's first scale puts its largest magnitude into [2^7, 2^8), so that
 // it and what rounding leaves of it, at most 2^3, stay in range (448); the next plane holds sixteen times the remainder with a scale
-// of a sixteenth, and so on.  With two planes all bf16 numbers down to 2^-14 of the block's largest come out exactly (eight bits), and
-// what is lost of smaller ones is below 2^-21 of it; three planes do the same for fp16 (eleven bits).  Each remainder is exact in
-// fp32.  A block with an infinity or NaN gets the scale byte 255, which makes its products NaN.
+// of a sixteenth, and so on.  With two planes all bf16 numbers down to 2^-13 of the block's largest come out exactly (eight bits), and
+// what is lost of smaller ones is at most 2^-21 of it; three planes do the same for fp16 (eleven bits, 2^-25), five for fp32 (24 bits down to 2^-9,
+// 2^-33).  Scales end at 2^-127: of blocks that would need smaller ones up to 2^-137 is lost.  Each remainder is exact in fp32.  A block with an infinity or NaN gets the scale byte 255, which makes its products NaN.
 template <int NE>
 __device__ __forceinline__ void mx_to_planes(float (&v)[NE], bool there, uint8_t *blk, int act_bytes, int Mc, int planes, int m, int col) {
   uint32_t top = 0;
