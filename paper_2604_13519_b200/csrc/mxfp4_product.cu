@@ -640,12 +640,13 @@ template <int EPI>
 static cudaError_t prod_launch(const CUtensorMap &tw, const MxArgs &g, const MxPlan &p, size_t smem, cudaStream_t st, bool pdl) {
   if (p.stream) return prod_launch_one<EPI, kStream, 0, 0>(tw, g, p, smem, st, pdl);
   if (!p.own) return prod_launch_one<EPI, kTile, 0, 0>(tw, g, p, smem, st, pdl);
-  switch (g.x_type) {
-    case MX_BF16: return prod_launch_own<EPI, MX_BF16>(tw, g, p, smem, st, pdl);
-    case MX_F16: return prod_launch_own<EPI, MX_F16>(tw, g, p, smem, st, pdl);
-    case MX_PAIR: return prod_launch_own<EPI, MX_PAIR>(tw, g, p, smem, st, pdl);
-    default: return prod_launch_own<EPI, MX_F32>(tw, g, p, smem, st, pdl);
+  if (g.x_type == MX_BF16) return prod_launch_own<EPI, MX_BF16>(tw, g, p, smem, st, pdl);
+  if (g.x_type == MX_PAIR) return prod_launch_own<EPI, MX_PAIR>(tw, g, p, smem, st, pdl);
+  if constexpr (EPI == MX_STORE) {   // (a model's activations are of the two types above)
+    if (g.x_type == MX_F16) return prod_launch_own<EPI, MX_F16>(tw, g, p, smem, st, pdl);
+    if (g.x_type == MX_F32) return prod_launch_own<EPI, MX_F32>(tw, g, p, smem, st, pdl);
   }
+  return cudaErrorInvalidValue;
 }
 
 MxOut mx_out(int n_kb, int planes, void *scratch, const MxPlan &p) {
