@@ -202,7 +202,8 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tw, const MxArgs g) {
     // ------------------------------------------------------------------ copies
     // The whole warp walks the loop; one elected lane issues a stage's copies (from a lane in a branch of its own each takes twice as
     // long, and this warp's time per stage is what bounds a CTA).
-    // (weights that every chunk reads again stay in L2: 1024 x 24576 x 4096 176 -> 165 us, call after call 210 -> 190)
+    // (weights that every chunk reads again stay in L2, us a call: 301 x 4096 x 12288 of fp16 64.4 -> 60.0, 57 x 5003 x 4100 of fp32 14.9 -> 14.0,
+    // but 1024 x 24576 x 4096 224.7 -> 226.5)
     const uint64_t pol_w = g.chunks > 1 ? policy_evict_normal() : policy_evict_first(), pol_a = policy_evict_last();
     const int n = (int)(u1 - u0), x_block = act_bytes + 512 * sb_words;
     auto load_w = [&](uint32_t dst, uint32_t bar, int blk) {
@@ -322,63 +323,26 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tw, const MxArgs g) {
     const int f = q * 32 + lane;                  // this thread's feature of a tile
     const uint32_t stg = smem_u32(staging);
     pdl_wait();   // (flags are cleared by the kernel before; outputs may still be read by its consumers)
-    if (EPI == MX_SWIGLU && blockIdx.x == 0 && warp == 2) mx_clear_flags(g.mo, lane, 32);
+    if (EPI == MX_SWIGLU && cta == 0 && warp == 2) mx_clear_flags(g.mo, lane, 32);
     int j = 0, turn = 0;
     bool alive = true;   // (all warps go through the same barriers whatever becomes of a wait; after one has expired none is waited for)
     for (long long hi = u1; hi > u0; ++j) {
       const ProdSeg t = prod_seg(g, u0, hi);
       hi -= t.kb1 - t.kb0;
       const int b = n_acc == 2 ? j & 1 : 0, use = n_acc == 2 ? j >> 1 : j;
-      const int tile = t.item / g.chunks, z = t.item % g.chunks, m0 = z * g.Mc, M = min(g.Mc, g.M - m0);
-      const bool finish = t.kb1 == g.n_kb;   // else another CTA finishes the tile
-      int before = cta;                      // CTAs [before, cta) have its earlier k-blocks
-      bool there = true;                     // their partial sums are
-      if (finish && t.kb0 > 0) {
-        const long long first = (long long)t.item * g.n_kb;
-        do --before;
-        while (prod_start(g, before, G) > first);
-        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, ld_acquire(g.flags + c));
-      }
-      // The CTAs' partial sums, 32 rows ahead of use: the first of them are under way while the tile's last products run, unless they are late (as
-      // they are where a run is shorter than a tile).
-      float part[4][8];
-      auto fetch = [&](int c0, float (&p)[8]) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = 0.f;
-        for (int c = before; there && c0 < M && c < cta; ++c) {
-          const float *slab = g.slabs + ((size_t)c * g.Mc + c0) * kMxTileN + f;
-          if (c == before) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = __ldcg(slab + i * kMxTileN);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] += __ldcg(slab + i * kMxTileN);
-          }
-        }
-      };
-      if (there) {
-#pragma unroll
-        for (int h = 0; h < 4; ++h) fetch(8 * h, part[h]);
-      }
       bool ok = alive && __all_sync(0xffffffffu, mbar_wait(smem_u32(&ctl->acc_full[b]), use & 1));
-      if (alive && !ok && lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
+      if (!ok && lane == 0) prod_error(g, DEV_TIMEOUT_TMEM);
       alive = ok;
-      if (!there) {
-        there = ok;
-        for (int c = before; there && c < cta; ++c) there = __all_sync(0xffffffffu, wait_flag(g.flags + c));
-        if (ok && !there && lane == 0) prod_error(g, DEV_TIMEOUT_GRID);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) fetch(8 * h, part[h]);
-      }
       tc_fence_after();
-      ok = ok && there && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
+      ok = ok && (*reinterpret_cast<volatile uint32_t *>(&ctl->abort_flag) == 0);
+      const int tile = t.item / g.chunks, z = t.item - tile * g.chunks, m0 = z * g.Mc, M = min(g.Mc, g.M - m0);
       const uint32_t taddr = tmem_base + b * acc_cols + ((uint32_t)(q * 32) << 16);
       auto emptied = [&]() {   // the sums are out of tensor memory
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[b]));
       };
-      if (!finish) {
+      if (t.kb1 != g.n_kb) {   // another CTA finishes the tile
         float *slab = g.slabs + (size_t)cta * g.Mc * kMxTileN + f;
         for (int c0 = 0; c0 < M; c0 += 8) {
           float v[8];
@@ -393,26 +357,42 @@ mx_product_kernel(const __grid_constant__ CUtensorMap tw, const MxArgs g) {
         if (warp == 2 && lane == 0 && ok) asm volatile("st.release.gpu.global.b32 [%0], %1;" ::"l"(g.flags + cta), "r"(1) : "memory");
         continue;
       }
+      int before = cta;   // CTAs [before, cta) have its earlier k-blocks
+      if (t.kb0 > 0) {
+        const long long first = (long long)t.item * g.n_kb;
+        do --before;
+        while (prod_start(g, before, G) > first);
+        for (int c = before; ok && c < cta; ++c) ok = __all_sync(0xffffffffu, wait_flag(g.flags + c));
+        if (!ok && lane == 0) prod_error(g, DEV_TIMEOUT_GRID);
+      }
+      float part[8];   // the CTAs' partial sums, eight rows ahead of use
+      auto fetch = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[i] = 0.f;
+        for (int c = before; ok && c0 < M && c < cta; ++c) {
+          const float *slab = g.slabs + ((size_t)c * g.Mc + c0) * kMxTileN + f;
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = __ldcg(slab + i * kMxTileN);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) part[i] += x[i];
+        }
+      };
+      fetch(0);
       const int n = tile * kMxTileN + lane * 4;
-      for (int r0 = 0; r0 < M; r0 += 32) {
+      for (int c0 = 0; c0 < M; c0 += 8, turn ^= 1) {
+        const uint32_t buf = stg + turn * (kProdStaging / 2);
+        float v[8];
+        prod_sums(g, taddr + c0, v);
+        if (c0 + 8 >= M) emptied();
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          const int c0 = r0 + 8 * h;
-          if (c0 >= M) break;
-          const uint32_t buf = stg + turn * (kProdStaging / 2);
-          turn ^= 1;
-          float v[8];
-          prod_sums(g, taddr + c0, v);
-          if (c0 + 8 >= M) emptied();
-#pragma unroll
-          for (int i = 0; i < 8; ++i) st_shared_f32(buf + (i * kMxTileN + f) * 4, v[i] + part[h][i]);
-          fetch(c0 + 32, part[h]);
-          asm volatile("bar.sync 2, 128;" ::: "memory");
-          for (int i = q; ok && i < 8 && c0 + i < M; i += 4) {
-            const uint4 u = ld_shared_v4(buf + (i * kMxTileN + lane * 4) * 4);
-            const float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
-            mx_finish<EPI>(g, g.row0 + m0 + c0 + i, n, w, lane);
-          }
+        for (int i = 0; i < 8; ++i) st_shared_f32(buf + (i * kMxTileN + f) * 4, v[i] + part[i]);
+        fetch(c0 + 8);
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        for (int i = warp - 2; ok && i < 8 && c0 + i < M; i += 4) {
+          const uint4 u = ld_shared_v4(buf + (i * kMxTileN + lane * 4) * 4);
+          const float w[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+          mx_finish<EPI>(g, g.row0 + m0 + c0 + i, n, w, lane);
         }
       }
     }
@@ -531,9 +511,11 @@ static size_t prod_stage_bytes(int planes, int Mc) { return kProdW + ((512 + mx_
 // own.
 //
 // Runs where there are more tiles than places, and where tiles do not come out even over the SMs and the time that costs is worth the
-// second exchange at a run's end, 7 to 12 us: 64 rows x 20480 x 12288, 160 tiles, 51 -> 46 us; 64 rows x 24576 x 4096, 192 tiles, 21
-// and 28.  (An SM takes a block in about 256 + 2 x columns cycles, the time of its bytes through shared memory: weights 16 KB, columns x 128, all of it
-// written and read, 128 a cycle.  The rule counts 32 columns: with 224, 112 rows x 20480 x 8192 took 56 us in runs and 54 in tiles.)
+// second exchange at a run's end, 4 to 8 us (device time, tiles and runs): 20480 x 12288, 160 tiles, 1 row 32.8 and 29.1 us, 32 rows 39.7 and 35.1,
+// 64 rows 47.3 and 41.5; 20480 x 8192 22.9 and 23.2, 28.3 and 28.1, 34.2 and 35.0; 24576 x 4096, 192 tiles, 13.8 and 18.4, 17.8 and 22.2, 21.3 and 28.2;
+// 112 rows x 20480 x 8192 50.1 and 48.0, 301 fp16 rows x 4096 x 12288 65.8 and 50.1, 112 x 24576 x 4096 30.0 and 38.0.  (An SM takes a block in about
+// 256 + 2 x columns cycles, the time of its bytes through shared memory: weights 16 KB, columns x 128, all of it written and read, 128 a
+// cycle.  Up to 64 rows the rule may not see how many there are and counts 32 columns.)
 // Rows whose planes the product makes itself: up to two, and up to four where a CTA has few blocks (its warps make a block of four rows in
 // about as long as a block of two takes to be multiplied; 4096 x 4096 at 4 rows 8.4 -> 6.5 us, 24576 x 4096 at 3 rows 15.4 and 17.1).
 // Up to eight bf16 rows take as long that way as with a launch for the planes (2048 x 8192 at 8 rows 9.0 and 8.9 us; fp16 9.5 and 8.8, fp32 11.5
@@ -555,7 +537,7 @@ MxPlan mx_plan(int M, int tiles, int n_kb, int planes, int n_sms, const int *fit
   n_sms = std::min(n_sms, kMxMostSms);
   const bool same = M <= (planes == 5 ? 32 : 64);
   const long long items = (long long)tiles * (same ? 1 : p.chunks), places = (long long)kProdCtas * n_sms;
-  const long long uneven = ((items + n_sms - 1) / n_sms * n_sms - items) * n_kb * (256 + 2 * 32) / n_sms;
+  const long long uneven = ((items + n_sms - 1) / n_sms * n_sms - items) * n_kb * (256 + 2 * (same ? 32 : planes * p.Mc)) / n_sms;
   p.apart = same && p.chunks > 1;
   p.stream = items > n_sms && items * n_kb >= 4 * places && ((items > places && (same || p.chunks == 1)) || uneven > kRunCycles);
   // (A tenth more than are needed must fit: how many do depends on how the device's SMs are grouped, and one that finds its place taken runs
