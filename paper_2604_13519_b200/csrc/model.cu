@@ -222,8 +222,9 @@ void make_layout(const ts_model_config &c, Layout *L) {
   L->mx = L->mx2 = 0;
   if (c.weights == TS_WEIGHTS_MXFP4) {   // planes of the projections' inputs (of `down` apart), sums of tiles that two CTAs share
     const int planes_mx = ts::mx_planes_of(c.act_split ? ts::MX_PAIR : ts::MX_BF16);
-    L->mx = take(ts::mx_scratch_most((int)R, (int)((std::max(d, Nq) + ts::kMxTileK - 1) / ts::kMxTileK), planes_mx));
-    L->mx2 = take(ts::mx_scratch_most((int)R, (int)((F + ts::kMxTileK - 1) / ts::kMxTileK), planes_mx));
+    const auto blocks = [](uint64_t side, int of) { return (int)((side + of - 1) / of); };
+    L->mx = take(ts::mx_scratch_most((int)R, blocks(std::max({V, 2 * F, (uint64_t)L->Nqkv, d}), ts::kMxTileN), blocks(std::max(d, Nq), ts::kMxTileK), planes_mx));
+    L->mx2 = take(ts::mx_scratch_most((int)R, blocks(d, ts::kMxTileN), blocks(F, ts::kMxTileK), planes_mx));
   }
   L->workspace_bytes = o;
   L->host_io_bytes = align_up((uint64_t)(L->in_ints + L->out_ints + 2 * ts::kTopMax + 2) * 4, 4096);   // (and a retrieval's result pairs, status and number)

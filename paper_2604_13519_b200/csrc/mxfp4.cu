@@ -547,8 +547,7 @@ ts_status ts_mxfp4_product_workspace(int64_t rows, int64_t n, int64_t k, int32_t
   MX_OK(matrix_ok(n, k));
   MX_OK(matrix_ok(rows, k));
   if (!type_ok(x_type)) return set_error(TS_ERR_ARG, "unknown element type %d", x_type);
-  *bytes = 0;
-  if (n) *bytes = ts::mx_scratch_most((int)rows, (int)kblocks_of(k), ts::mx_planes_of(x_type));
+  *bytes = ts::mx_scratch_most((int)rows, (int)tiles_of(n), (int)kblocks_of(k), ts::mx_planes_of(x_type));
   return TS_OK;
 }
 

@@ -244,8 +244,8 @@ struct MxInput {
 };
 struct MxScratch { uint64_t flags, slabs, bytes; };
 MxScratch mx_scratch(int n_kb, int planes, const MxPlan &p);
-// Enough for products with matrices of `n_kb` k-blocks or fewer with up to `rows` rows, whatever their features and the device.
-uint64_t mx_scratch_most(int rows, int n_kb, int planes);
+// Enough for products with matrices of `tiles` x `n_kb` blocks or fewer with up to `rows` rows, whatever the device.
+uint64_t mx_scratch_most(int rows, int tiles, int n_kb, int planes);
 constexpr int kMxMostSms = 256;
 // whether rows of 16- or 32-bit elements can be read 16 bytes at a time
 inline bool mx_aligned(const void *p, long long ld, int type) { return ((uintptr_t)p & 15) == 0 && ld * (type == MX_F32 ? 4 : 2) % 16 == 0; }

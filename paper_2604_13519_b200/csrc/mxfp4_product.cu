@@ -559,15 +559,17 @@ MxScratch mx_scratch(int n_kb, int planes, const MxPlan &p) {
   w.bytes = w.slabs + (p.stream ? (uint64_t)p.ctas * p.Mc * kMxTileN * 4 : 0);
   return w;
 }
-uint64_t mx_scratch_most(int rows, int n_kb, int planes) {
-  if (!rows || !n_kb) return 0;
+uint64_t mx_scratch_most(int rows, int tiles, int n_kb, int planes) {
+  if (!rows || !tiles || !n_kb) return 0;
   MxPlan p = mx_cut(rows, planes);
   if (p.chunks > 1) {   // (equal chunks may be larger for fewer rows)
     p.Mc = kProdAcc / planes / mx_step(planes) * mx_step(planes);
     p.chunks = (rows + p.Mc - 1) / p.Mc;
   }
-  p.stream = p.apart = true;
-  p.ctas = kProdCtas * kMxMostSms;
+  // (mx_plan deals out in runs where there are more items than SMs, and four k-blocks or more for each of the CTAs, two to an SM)
+  const long long items = (long long)tiles * p.chunks;
+  p.ctas = (int)std::min({(long long)kProdCtas * kMxMostSms, kProdCtas * (items - 1), items * n_kb / 4});
+  p.stream = p.apart = p.ctas > 0;
   return mx_scratch(n_kb, planes, p).bytes;
 }
 

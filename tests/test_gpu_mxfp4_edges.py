@@ -124,3 +124,21 @@ def test_results_of_every_type_are_the_same_sums_rounded(m, n, k, x_type):
             assert torch.equal(y, sums.to(dtype))
             y.fill_(77.0)
             assert (full == 77).all()
+
+
+@pytest.mark.parametrize("x_type", TYPES)
+@pytest.mark.parametrize("rows,n,k", [(70, 200, 4100), (300, 1000, 700), (130, 19000, 1100), (66, 38100, 700), (9, 38100, 1000)])
+def test_a_workspace_serves_fewer_rows_too(rows, n, k, x_type):
+    """Exactly as much memory as is asked for, and behind it a guard that stays as it is."""
+    rng = np.random.default_rng(rows)
+    codes = torch.from_numpy(rng.integers(0, 256, (n, 16 * ((k + 31) // 32)), dtype=np.uint8)).cuda()
+    w = ts.Mxfp4Matrix(codes, torch.full((n, (k + 31) // 32), 120, dtype=torch.uint8, device="cuda"), k)
+    x = torch.randn(rows, k, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(TYPES[x_type])
+    size = w.workspace(rows, TYPES[x_type]).numel()
+    held = torch.full((size + 4096,), 123, dtype=torch.uint8, device="cuda")
+    for m in sorted({1, 3, 8, rows // 4, rows // 2, rows - 1, rows}):
+        if m:
+            y = ts.ts_mxfp4_product(w, x[:m], torch.float32, workspace=held[:size])
+            assert torch.equal(y, ts.ts_mxfp4_product(w, x[:m].clone(), torch.float32))
+    w.check()
+    assert (held[size:] == 123).all()

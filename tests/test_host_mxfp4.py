@@ -132,3 +132,25 @@ def test_model_configuration_refuses():
     c.path, c.weights = 0, 2
     _refused(L.ts_query_buffer_sizes(C.byref(c), C.byref(out)), "weights")
     _refused(L.ts_load_tensor_mxfp4(None, 3, 0, P, P, 4, 64), "null")
+
+
+def test_workspaces_are_no_larger_than_the_matrix_can_need():
+    """Partial sums take memory only where a matrix has tiles enough to be dealt out in runs, and then for no more CTAs than it has work for."""
+    L, out = B.lib(), C.c_uint64()
+
+    def size(*a):
+        assert L.ts_mxfp4_product_workspace(*a, C.byref(out)) == 0
+        return out.value
+    planes = lambda rows, k, n: n * (rows + 112) * (k + 127) // 128 * 128 * 2       # (elements; scales and rounding up: twice that)
+    assert size(3, 128, 128, 0) <= planes(3, 128, 2)
+    assert size(256, 256, 256, 0) <= planes(256, 256, 2)
+    assert size(256, 1024, 4096, 2) <= planes(256, 4096, 5) + 24 * 32 * 512 * 16
+    assert size(64, 151936, 4096, 0) <= planes(64, 4096, 2) + 512 * 112 * 512 + 4096
+    for x_type in (0, 1, 2):
+        for k in (1, 128, 300, 4100):
+            for rows in (1, 64, 300, 2000):
+                most = 0
+                for n in (1, 100, 128, 129, 1000, 4096, 19000, 38000, 151936):
+                    b = size(rows, n, k, x_type)
+                    assert b >= most
+                    most = b
