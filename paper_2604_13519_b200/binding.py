@@ -307,6 +307,8 @@ class Model:
     def load_tensor_mxfp4(self, kind: int, layer: int, codes, scales, cols: int):
         """codes, scales: uint8 tensors as ts_mxfp4_quantise returns them, of a matrix of `cols` columns (host or device)."""
         nb, rows = (cols + 31) // 32, codes.shape[0]
+        if codes.element_size() != 1 or scales.element_size() != 1:
+            raise ValueError("codes and scales must be uint8 tensors")
         if tuple(codes.shape) != (rows, 16 * nb) or tuple(scales.shape) != (rows, nb):
             raise ValueError(f"{cols} columns take codes of [rows][{16 * nb}] and scales of [rows][{nb}]")
         codes, scales = codes.contiguous(), scales.contiguous()

@@ -154,3 +154,12 @@ def test_workspaces_are_no_larger_than_the_matrix_can_need():
                     b = size(rows, n, k, x_type)
                     assert b >= most
                     most = b
+
+
+def test_a_model_takes_codes_and_scales_of_one_byte_each():
+    torch = pytest.importorskip("torch")
+    m = B.Model.__new__(B.Model)      # (refused before anything is asked of a model)
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)
+    for codes, scales in ((u8(4, 32).int(), u8(4, 2)), (u8(4, 32), u8(4, 2).short()), (u8(4, 32).float(), u8(4, 2)), (u8(128), u8(8)), (u8(4, 32), u8(8))):
+        with pytest.raises(ValueError):
+            m.load_tensor_mxfp4(B.TS_W_Q, 0, codes, scales, 64)
