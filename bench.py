@@ -595,6 +595,13 @@ def main():
                     "unit": "GB/s", "frac": gbs / peaks["hbm_gbs"], "traffic": None,
                     "peak_source": peaks["source"], "bytes_per_launch": ab["total"], "ms_per_launch": ms,
                     "phase_ms": {k: v[0] for k, v in prof.items() if k in ("gemm", "attention", "attention_merge")}}
+    elif args.weights == "mxfp4":
+        # products with MXFP4 matrices, and what prepares their input where no other kernel leaves it: the matrices once
+        gemm_ms, gemm_n = prof["gemm"]
+        gbs = ab["weights"] / (gemm_ms * 1e-3) / 1e9
+        roofline = {"bound": "hbm", "kernel": "mx_product_kernel", "achieved": gbs, "peak": peaks["hbm_gbs"], "unit": "GB/s",
+                    "frac": gbs / peaks["hbm_gbs"], "traffic": None, "peak_source": peaks["source"],
+                    "bytes_per_launch": ab["weights"] / gemm_n, "ms_per_launch": gemm_ms / gemm_n}
     else:
         gemm_bytes, gemm_launches = gemm_bytes_per_step(shape, M, planes)
         gemm_ms, gemm_n = prof["gemm"]
@@ -646,8 +653,6 @@ def main():
                "sample": f"one chunk forward over the first {nl} of {shape.n_layers} layers + LM head on the same "
                          f"shapes, layer time scaled to full depth ({sec:.1f} s per step)"}
 
-    if args.weights != "bf16":
-        roofline = None     # (of the bf16 projections' kernel)
     if rank == 0:
         out = {
             "metric": METRIC, "value": world * M / (ms * 1e-3), "unit": UNIT, "n_gpus": world, "steps": args.steps,
