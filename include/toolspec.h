@@ -409,7 +409,7 @@ ts_status ts_debug_schedule(int32_t n_tiles, int32_t n_kblocks, int32_t n_ctas, 
  * (nanoseconds of the GPU's global timer): earliest CTA start, earliest and latest return from the dependency wait,
  * latest CTA end.  stamps: host, 4 values per launch in launch order; classes: host, the launch's class as in
  * ts_profile_step; at most cap launches are written, *n_launches receives their number.  A launch without stamps
- * (acceptance, Top-K, sampling) reports ~0, ~0, 0, 0.  One-kernel-per-stage path only.  Synchronises the stream. */
+ * (acceptance, Top-K, sampling, a kernel of its own that prepares the input of an MXFP4 product) reports ~0, ~0, 0, 0.  One-kernel-per-stage path only.  Synchronises the stream. */
 ts_status ts_debug_timeline(ts_model *m, uint64_t *stamps, int32_t *classes, int32_t cap, int32_t *n_launches);
 /* Make the NEXT step or retrieval (ts_verify*, ts_prefill, ts_topk_cosine) report `code` (> 0) in its device status word,
  * as a bounded device-side wait that expired would: the word is written on the model's stream behind the step's last

@@ -672,6 +672,7 @@ cudaError_t launch_mx_product(int epi, const CUtensorMap &tw, MxArgs g, const Mx
       case MX_LOGITS: e = prod_launch<MX_LOGITS>(tw, g, p, smem, st, pdl); break;
     }
     if (e != cudaSuccess) return e;
+    if (g.stamp) g.stamp += 4;   // (the next launch's)
   }
   if (launches) *launches = passes;
   return cudaSuccess;

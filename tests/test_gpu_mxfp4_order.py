@@ -107,3 +107,21 @@ def test_check_waits_for_products_on_every_stream():
         w.check()
     assert e.value.code == -6 and "code 3" in str(e.value)
     w.check()
+
+
+def test_every_launch_of_a_product_is_in_the_timeline():
+    """60 rows through an LM head of many tiles: the product takes two launches, each with stamps of its own."""
+    shape = ModelShape("wide-head-1l", 1, 512, 8, 4, 64, 1024, 38016, 10000.0, 1e-5)     # 297 tiles
+    gm = ts.Model(shape, max_pages=40, max_batch=1, k_max=64, max_rows=64, max_ctx=400, weights="mxfp4")
+    gm.load_weights(synth.make_weights(shape))
+    gm.kv_pool_tensor().zero_()
+    s = ts.Session(gm, None, None)
+    s.set_cache(200, 70)
+    ts.ts_verify(gm, [s], [_draft(shape.vocab, 59, 2)])
+    products = [t for t in gm.timeline() if t[0] == "gemm"]
+    assert len(products) == ts.ts_profile_step(gm)["gemm"][1] == 4 * shape.n_layers + 2
+    for _, start, first, last, end in products:
+        assert start <= first <= last <= end
+    assert products[-2][4] <= products[-1][2] and products[-2][4] < products[-1][4]      # (the second of the two waits for the first one's end)
+    s.close()
+    gm.close()
