@@ -728,8 +728,9 @@ def ts_mxfp4_dequantise(codes, scales, cols: int, dtype, out=None, stream=None):
 
 
 class Mxfp4Matrix:
-    """An MXFP4 matrix [n][k] in the form that ts_mxfp4_product reads, laid out from codes and scales (which it does not keep).  The
-    constructor returns when it is laid out, so that products may run on any stream; it cannot be captured."""
+    """An MXFP4 matrix [n][k] in the form that ts_mxfp4_product reads, laid out from codes and scales (which it does not keep).  It is
+    laid out on `stream`, behind what the current stream has to do, and the constructor returns when that is done, so that products may run on
+    any stream; it cannot be captured."""
 
     def __init__(self, codes, scales, k: int, stream=None):
         import torch
@@ -738,6 +739,7 @@ class Mxfp4Matrix:
         size = C.c_uint64()
         _check(lib().ts_mxfp4_matrix_bytes(self.n, k, C.byref(size)))
         where = stream if stream is not None else torch.cuda.current_stream(self.device)
+        where.wait_stream(torch.cuda.current_stream(self.device))     # (which may be making codes and scales)
         with torch.cuda.stream(where):
             self.data = torch.empty(size.value, dtype=torch.uint8, device=self.device)
             self.status = torch.zeros(1, dtype=torch.int32, device=self.device)

@@ -125,3 +125,23 @@ def test_every_launch_of_a_product_is_in_the_timeline():
     assert products[-2][4] <= products[-1][2] and products[-2][4] < products[-1][4]      # (the second of the two waits for the first one's end)
     s.close()
     gm.close()
+
+
+def test_a_matrix_is_laid_out_behind_what_makes_its_codes():
+    """Codes and scales that the current stream is still to write, laid out on another one."""
+    n, k = 512, 1024
+    gen = torch.Generator("cuda").manual_seed(3)
+    packs = [(torch.randint(0, 256, (n, k // 2), dtype=torch.uint8, device="cuda", generator=gen),
+              torch.randint(118, 122, (n, k // 32), dtype=torch.uint8, device="cuda", generator=gen)) for _ in range(2)]
+    x = torch.randn(5, k, device="cuda", generator=gen).to(torch.bfloat16)
+    want = [ts.ts_mxfp4_product(ts.Mxfp4Matrix(*p, k), x, torch.float32) for p in packs]
+    codes, scales = packs[0][0].clone(), packs[0][1].clone()
+    side = torch.cuda.Stream()
+    ts.Mxfp4Matrix(codes, scales, k, stream=side)      # (memory of that stream, for the next one)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    codes.copy_(packs[1][0])
+    scales.copy_(packs[1][1])
+    w = ts.Mxfp4Matrix(codes, scales, k, stream=side)
+    assert torch.equal(ts.ts_mxfp4_product(w, x, torch.float32), want[1])
+    w.check()
